@@ -398,6 +398,104 @@ int moe_layer_forward(const ew_layer* layer, const void* x, const int32_t* adapt
                       float eps, void* stream);
 
 /* ===================================================================================== *
+ * The experts' products one by one, with their gradients, and experts held in 4 bits
+ *
+ * All of them take rows as the permutation leaves them: sorted by slot, slot s with counts[s] rows from row
+ * offsets[s] on, row r made from pair pair_of_row[r] (NULL: pair r), that is from token pair / k.
+ * num_rows is the room that the row arrays have; offsets[P] <= num_rows rows exist, and rows behind the last
+ * one are neither read nor written.  A slot without rows is never dereferenced.  Nothing is kept between
+ * calls and no call needs scratch of its own unless it takes a workspace; results do not depend on the
+ * launch (no atomics), so calls repeat bit for bit, also out of a captured graph.
+ * ===================================================================================== */
+
+/* Matrix products grouped by expert (Sec. 2.1: the grouped matrix multiplication), for row r of slot s:
+ *   transposed == 0:  y[r][n] = sum_k x[t][k] * w_base[s][n][k],   w_base [P, N, K]
+ *   transposed != 0:  y[r][n] = sum_k x[t][k] * w_base[s][k][n],   w_base [P, K, N]
+ * with t = pair_of_row[r] / k.  The second form is the input gradient of the first: dx = dy W takes
+ * x = dy (sorted rows: pair_of_row NULL, k = 1), K = the forward product's N and N = its K.
+ *   x [dev] dtype [*, K]; y [dev] dtype [num_rows, N]
+ * fp32 accumulation, rounded once into y.  Any K and N; bf16 runs on the bf16 matrix cores where K and N are
+ * multiples of 8, x, w_base and y are aligned to 16 bytes and a slot's weights and the rows of x are
+ * addressable with 32-bit byte offsets, and in fp32 otherwise.
+ * num_rows = 0 is a no-op.  Errors: INVALID_ARG, UNSUPPORTED (a launch of 2^31 workgroups), HIP. */
+int moe_grouped_gemm(const void* x, int dtype, int num_rows, int k, int K, int N, int P, int transposed,
+                     const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
+                     const void* w_base, void* y, void* stream);
+
+/* Weight gradients of moe_grouped_gemm (transposed == 0) for slots first_slot .. first_slot+num_slots-1:
+ *   dw[s - first_slot][n][k] (+)= sum over the rows r of slot s of dy[r][n] * x[pair_of_row[r] / k][k]
+ *   dy [dev] dtype [num_rows, N]; x [dev] dtype [*, K]
+ *   dw [dev] dw_dtype [num_slots, N, K]: EW_F32, or EW_BF16 for bf16 rows (rounded once).  accumulate != 0
+ *      adds to what dw holds (EW_F32 only); otherwise slots without rows get zeros.
+ * A product w of the second form (transposed != 0) has the same gradient with dy and x exchanged.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_rows, int k, int K, int N, int P,
+                           const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
+                           int first_slot, int num_slots, int dw_dtype, int accumulate, void* dw,
+                           void* stream);
+
+/* Gradients of moe_grouped_ffn: from dy (of y_sorted) those of the rows' inputs and of the weights of slots
+ * first_slot .. first_slot+num_slots-1 (an adapter's slots, or all).  With g = W1g x, u = W1u x, s = sigmoid(g):
+ *   da = W2^T dy, dg = da u s (1 + g (1 - s)), du = da g s, a = g s u
+ *   dx_sorted[r] = W1g^T dg + W1u^T du;  dw13 (+)= sum_r [dg; du] x^T;  dw2 (+)= sum_r dy a^T
+ *   x [dev] dtype [*, H]; dy [dev] dtype [num_rows, H]; w13_base, w2_base as for moe_grouped_ffn
+ *   dx_sorted [dev] dtype [num_rows, H], one row per pair, or NULL.  A token's input gradient is the sum over its
+ *      pairs: moe_unpermute(dx_sorted, row_of_pair, ones).
+ *   dw13 [dev] dw_dtype [num_slots, 2I, H], dw2 [dev] dw_dtype [num_slots, H, I], either may be NULL;
+ *      dw_dtype and accumulate as for moe_grouped_gemm_wgrad
+ * g and u are computed again.  bf16: g, u, da, dg, du and a are bf16 between the products.
+ * Any H and I (what runs on the bf16 matrix cores: as moe_grouped_gemm).
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
+size_t moe_grouped_ffn_backward_workspace_bytes(int num_rows, int I, int dtype);
+int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype, int num_rows, int k, int H, int I, int P,
+                             const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
+                             const void* w13_base, const void* w2_base, void* dx_sorted, int first_slot,
+                             int num_slots, int dw_dtype, int accumulate, void* dw13, void* dw2, void* ws,
+                             size_t ws_bytes, void* stream);
+
+/* Gradients of moe_unpermute with respect to the expert outputs and the router weights, for p = t*k + j:
+ *   dy_sorted[row_of_pair[p]] = topk_w[t, j] * dout[t];  dw[t, j] = <dout[t], y_sorted[row_of_pair[p]]>
+ * (shared experts' outputs and the residual have dout itself as their gradient).
+ *   dout [dev] dtype [T, H]; y_sorted, dy_sorted [dev] dtype [T*k, H]; dw [dev] float32 [T, k]
+ *   y_sorted and dw are both given or both NULL.
+ * T = 0 is a no-op.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+int moe_unpermute_backward(const void* dout, const void* y_sorted, const int32_t* row_of_pair,
+                           const float* topk_w, int T, int k, int H, int dtype, void* dy_sorted, float* dw,
+                           void* stream);
+
+/* Experts in 4 bits: E2M1 values (0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign) of which 32 neighbours along K share a
+ * scale 2^(byte - 127) (255: NaN), the OCP Microscaling format.  An expert's [N, K] weights are one run of
+ * moe_w4_expert_bytes(N, K) = 17/32 N K bytes: codes [N, K/2], the even element in the low half of a byte, then
+ * scales [N, K/32].  That number is also what expert_pool_create is given for a pool of such experts: pages,
+ * adapters and the expert map know nothing of the format.  0: sizes that cannot be packed (K % 32, N*K % 512). */
+size_t moe_w4_expert_bytes(int N, int K);
+
+/* w [dev] dtype [num_experts, N, K] -> out [dev] [num_experts, moe_w4_expert_bytes(N, K)]: the scale is
+ * 2^(floor(log2 m) - 2), m the largest magnitude of the group (at least 2^-127); values round to the nearest
+ * code, halves to the even one, and beyond 6 to 6.  A group with an infinity or a NaN becomes NaN.
+ * moe_dequantize_w4 writes the values that the codes stand for; both types hold them exactly (codes beyond
+ * the types' range, with scales of 253 and 254, give infinities).
+ * Pointers aligned to 16 bytes.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+int moe_quantize_w4(const void* w, int dtype, int num_experts, int N, int K, void* out, void* stream);
+int moe_dequantize_w4(const void* w4, int dtype, int num_experts, int N, int K, void* w, void* stream);
+
+/* moe_grouped_gemm (transposed == 0) and moe_grouped_ffn with 4-bit experts: x and the results bf16, weights
+ * exactly the values that the codes stand for, fp32 accumulation; the FFN's activation is rounded to bf16
+ * between its products.
+ *   w4_base [dev] [P, moe_w4_expert_bytes(N, K)]; w13_base [dev] [P, moe_w4_expert_bytes(2I, H)] (gate rows, then
+ *   up rows), w2_base [dev] [P, moe_w4_expert_bytes(H, I)]: a pool's tensors, or others.
+ * Limits: sizes that can be packed.  Fast where K is a multiple of 128 and N of 16 (the FFN: H and I of 128) and
+ * pointers are aligned to 16 bytes; plain otherwise.
+ * num_rows = 0 is a no-op.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
+int moe_grouped_gemm_w4(const void* x, int num_rows, int k, int K, int N, int P, const int32_t* counts,
+                        const int32_t* offsets, const int32_t* pair_of_row, const void* w4_base, void* y,
+                        void* stream);
+size_t moe_grouped_ffn_w4_workspace_bytes(int num_rows, int I);
+int moe_grouped_ffn_w4(const void* x, int num_rows, int k, int H, int I, int P, const int32_t* counts,
+                       const int32_t* offsets, const int32_t* pair_of_row, const void* w13_base,
+                       const void* w2_base, void* y_sorted, void* ws, size_t ws_bytes, void* stream);
+
+/* ===================================================================================== *
  * Measurement aids (not on the hot path): what the GPU sustains, timed by the caller with events
  * in the same run as the hot path, for quoting roofline fractions against achievable peaks.
  * ===================================================================================== */

@@ -58,6 +58,17 @@ SIGNATURES = {
     "moe_layer_forward": (_int, [_vp, _vp, _vp, _int, _vp, _vp, _vp, _vp, C.c_float, _vp]),
     "moe_gate_logits": (_int, [_vp, _int, _vp, _int, _int, _int, _vp, _vp, _vp, _vp]),
     "moe_rmsnorm": (_int, [_vp, _int, _int, _int, C.c_float, _vp, _vp]),
+    "moe_grouped_gemm": (_int, [_vp] + [_int] * 7 + [_vp] * 6),
+    "moe_grouped_gemm_wgrad": (_int, [_vp, _vp] + [_int] * 6 + [_vp] * 3 + [_int] * 4 + [_vp] * 2),
+    "moe_grouped_ffn_backward_workspace_bytes": (_sz, [_int, _int, _int]),
+    "moe_grouped_ffn_backward": (_int, [_vp, _vp] + [_int] * 6 + [_vp] * 6 + [_int] * 4 + [_vp] * 3 + [_sz, _vp]),
+    "moe_unpermute_backward": (_int, [_vp] * 4 + [_int] * 4 + [_vp] * 3),
+    "moe_w4_expert_bytes": (_sz, [_int, _int]),
+    "moe_quantize_w4": (_int, [_vp] + [_int] * 4 + [_vp] * 2),
+    "moe_dequantize_w4": (_int, [_vp] + [_int] * 4 + [_vp] * 2),
+    "moe_grouped_gemm_w4": (_int, [_vp] + [_int] * 5 + [_vp] * 6),
+    "moe_grouped_ffn_w4_workspace_bytes": (_sz, [_int, _int]),
+    "moe_grouped_ffn_w4": (_int, [_vp] + [_int] * 5 + [_vp] * 7 + [_sz, _vp]),
     "ew_probe_stream": (_int, [_vp, _vp, _sz, _int, _vp]),
     "ew_probe_mfma_bf16": (_int, [_int, _int, _int, _vp, _vp]),
     "ew_tune_ffn": (None, [_int, _int, _int, _int, _int, _int, _int]),
@@ -386,3 +397,188 @@ def moe_rmsnorm(x, eps: float = 1e-6, out=None):
     o = out if out is not None else torch.empty_like(x)
     _check(lib().moe_rmsnorm(_ptr(x), _dtype_code(x), T, H, float(eps), _ptr(o), _stream()))
     return o
+
+
+# ----------------------------------------------------------------------------- the experts' products one by one
+def _need(name, t, dtype, numel, like):
+    """Checks an operand: a contiguous tensor of this type on the device of `like`, with room for numel elements; or a raw
+    device pointer (a pool's tensor), or None."""
+    if t is None or isinstance(t, int):
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, is {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if t.numel() < numel:
+        raise ValueError(f"{name} has {t.numel()} elements, {numel} are needed")
+
+
+def _current(x):
+    """The device of x, which has to be the current one: kernels are enqueued on its current stream."""
+    if x.device.type != "cuda" or x.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {x.device}, not on the current HIP device")
+    return x.device
+
+
+def _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows):
+    """Number of sorted rows of a call, after checking what names them."""
+    if x.dim() != 2 or not x.is_contiguous():
+        raise ValueError("token rows must be a contiguous 2-D tensor")
+    _current(x)
+    rows = x.shape[0] * k if num_rows is None else num_rows
+    if pair_of_row is None and rows > x.shape[0] * k:
+        raise ValueError("more rows than pairs")
+    _need("counts", counts, torch.int32, P, x)
+    _need("offsets", offsets, torch.int32, P + 1, x)
+    _need("pair_of_row", pair_of_row, torch.int32, rows, x)
+    return rows
+
+
+def _result(name, out, shape, dtype, like):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    n = 1
+    for d in shape:
+        n *= d
+    _need(name, out, dtype, n, like)
+    return out
+
+
+def _scratch(ws, need, like):
+    if ws is None:
+        return _workspace(need, like.device)
+    _need("workspace", ws, torch.uint8, 0, like)
+    return ws
+
+
+def moe_grouped_gemm(x, k: int, N: int, P: int, counts, offsets, pair_of_row, w_base, transposed=False, out=None,
+                     num_rows: int | None = None):
+    """y[r] = W_s x[pair_of_row[r] / k] for the rows r of every slot s, w_base [P, N, K]; transposed: W_s^T, w_base [P, K, N] (the
+    input gradient: x = dy, k = 1, pair_of_row None).  w_base: a tensor or a raw device pointer (pool view).
+    num_rows defaults to x.shape[0] * k; returns y [num_rows, N], rows behind the last one as they were."""
+    rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
+    _need("w_base", w_base, x.dtype, P * N * K, x)
+    y = _result("out", out, (rows, N), x.dtype, x)
+    _check(lib().moe_grouped_gemm(_ptr(x), _dtype_code(x), rows, k, K, N, P, int(transposed), _ptr(counts), _ptr(offsets),
+                                  _ptr(pair_of_row), _ptr(w_base), _ptr(y), _stream()))
+    return y
+
+
+def moe_grouped_gemm_wgrad(dy, x, k: int, P: int, counts, offsets, pair_of_row, first_slot: int = 0, num_slots: int | None = None,
+                           dtype=torch.float32, accumulate=False, out=None):
+    """dW [num_slots, N, K] of moe_grouped_gemm from dy [rows, N] (sorted rows) and x [*, K], for the slots from first_slot on (all by
+    default); accumulate adds to `out` (float32)."""
+    if dy.dim() != 2 or not dy.is_contiguous() or dy.dtype != x.dtype or dy.device != x.device:
+        raise ValueError("dy must be a contiguous 2-D tensor of x's type and device")
+    rows, K, N = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0]), x.shape[1], dy.shape[1]
+    n = P - first_slot if num_slots is None else num_slots
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    dw = _result("out", out, (max(n, 0), N, K), dtype, x)
+    _check(lib().moe_grouped_gemm_wgrad(_ptr(dy), _ptr(x), _dtype_code(x), rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
+                                        first_slot, n, _dtype_code(dw), int(accumulate), _ptr(dw), _stream()))
+    return dw
+
+
+def moe_grouped_ffn_backward(x, dy, k: int, I: int, P: int, counts, offsets, pair_of_row, w13_base, w2_base, first_slot: int = 0,
+                             num_slots: int | None = None, dw_dtype=torch.float32, accumulate=False, want_dx=True, ws=None, dx=None,
+                             dw13=None, dw2=None):
+    """Gradients of moe_grouped_ffn from dy [rows, H]: (dx_sorted [rows, H], dw13 [num_slots, 2I, H], dw2 [num_slots, H, I]) for the
+    slots from first_slot on (all by default; num_slots = 0: none, then the weight gradients are None).  accumulate adds to dw13
+    and dw2 (float32).  A token's input gradient: moe_unpermute(dx_sorted, row_of_pair, ones)."""
+    if dy.dim() != 2 or not dy.is_contiguous() or dy.dtype != x.dtype or dy.device != x.device or dy.shape[1] != x.shape[1]:
+        raise ValueError("dy must be a contiguous [rows, H] tensor of x's type and device")
+    rows, H = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0]), x.shape[1]
+    n = P - first_slot if num_slots is None else num_slots
+    if accumulate and (dw13 is None or dw2 is None):
+        raise ValueError("accumulate needs dw13 and dw2")
+    _need("w13_base", w13_base, x.dtype, P * 2 * I * H, x)
+    _need("w2_base", w2_base, x.dtype, P * H * I, x)
+    dx = _result("dx", dx, (rows, H), x.dtype, x) if want_dx else None
+    if n > 0:
+        dw13 = _result("dw13", dw13, (n, 2 * I, H), dw_dtype, x)
+        dw2 = _result("dw2", dw2, (n, H, I), dw_dtype, x)
+    else:
+        dw13 = dw2 = None
+    ws = _scratch(ws, lib().moe_grouped_ffn_backward_workspace_bytes(rows, I, _dtype_code(x)), x)
+    _check(lib().moe_grouped_ffn_backward(_ptr(x), _ptr(dy), _dtype_code(x), rows, k, H, I, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
+                                          _ptr(w13_base), _ptr(w2_base), _ptr(dx), first_slot, n, EW_F32 if dw_dtype == torch.float32 else EW_BF16,
+                                          int(accumulate), _ptr(dw13), _ptr(dw2), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
+    return dx, dw13, dw2
+
+
+def moe_unpermute_backward(dout, row_of_pair, topk_w, y_sorted=None, out=None, dw_out=None):
+    """Gradients of moe_unpermute from dout [T, H]: (dy_sorted [T*k, H], dw [T, k]); dw is None without y_sorted."""
+    T, k = topk_w.shape
+    if dout.dim() != 2 or not dout.is_contiguous() or dout.shape[0] != T:
+        raise ValueError("dout must be a contiguous [T, H] tensor")
+    _current(dout)
+    H = dout.shape[1]
+    _need("row_of_pair", row_of_pair, torch.int32, T * k, dout)
+    _need("topk_w", topk_w, torch.float32, T * k, dout)
+    _need("y_sorted", y_sorted, dout.dtype, T * k * H, dout)
+    dy = _result("out", out, (T * k, H), dout.dtype, dout)
+    dw = _result("dw_out", dw_out, (T, k), torch.float32, dout) if y_sorted is not None else None
+    _check(lib().moe_unpermute_backward(_ptr(dout), _ptr(y_sorted), _ptr(row_of_pair), _ptr(topk_w), T, k, H, _dtype_code(dout), _ptr(dy),
+                                        _ptr(dw), _stream()))
+    return dy, dw
+
+
+# ----------------------------------------------------------------------------- experts in 4 bits
+def moe_w4_expert_bytes(N: int, K: int) -> int:
+    """Bytes of an expert's [N, K] weights in 4 bits: codes [N, K/2], then scales [N, K/32].  Also the size that ExpertPool takes for
+    a pool of such experts.  Raises for sizes that cannot be packed."""
+    n = lib().moe_w4_expert_bytes(N, K)
+    if n == 0:
+        raise EWError(-6, f"K must be a multiple of 32 and N*K of 512 (N={N} K={K})")
+    return n
+
+
+def moe_quantize_w4(w, out=None):
+    """w [E, N, K] (float32 or bfloat16) -> uint8 [E, moe_w4_expert_bytes(N, K)], what ExpertPool.map takes for a 4-bit pool."""
+    if w.dim() != 3 or not w.is_contiguous():
+        raise ValueError("w must be a contiguous [experts, N, K] tensor")
+    _current(w)
+    E, N, K = w.shape
+    o = _result("out", out, (E, moe_w4_expert_bytes(N, K)), torch.uint8, w)
+    _check(lib().moe_quantize_w4(_ptr(w), _dtype_code(w), E, N, K, _ptr(o), _stream()))
+    return o
+
+
+def moe_dequantize_w4(w4, N: int, K: int, dtype=torch.bfloat16, out=None):
+    """The values that packed experts uint8 [E, moe_w4_expert_bytes(N, K)] stand for, [E, N, K]."""
+    if w4.dim() != 2 or not w4.is_contiguous() or w4.dtype != torch.uint8 or w4.shape[1] != moe_w4_expert_bytes(N, K):
+        raise ValueError("w4 must be a contiguous uint8 [experts, moe_w4_expert_bytes(N, K)] tensor")
+    _current(w4)
+    o = _result("out", out, (w4.shape[0], N, K), dtype, w4)
+    _check(lib().moe_dequantize_w4(_ptr(w4), _dtype_code(o), w4.shape[0], N, K, _ptr(o), _stream()))
+    return o
+
+
+def moe_grouped_gemm_w4(x, k: int, N: int, P: int, counts, offsets, pair_of_row, w4_base, out=None, num_rows: int | None = None):
+    """moe_grouped_gemm with 4-bit experts: w4_base uint8 [P, moe_w4_expert_bytes(N, K)] or a raw device pointer; x bfloat16."""
+    if x.dtype != torch.bfloat16:
+        raise TypeError(f"token rows of 4-bit experts are bfloat16, not {x.dtype}")
+    rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
+    _need("w4_base", w4_base, torch.uint8, P * moe_w4_expert_bytes(N, K), x)
+    y = _result("out", out, (rows, N), x.dtype, x)
+    _check(lib().moe_grouped_gemm_w4(_ptr(x), rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row), _ptr(w4_base), _ptr(y), _stream()))
+    return y
+
+
+def moe_grouped_ffn_w4(x, k: int, I: int, P: int, counts, offsets, pair_of_row, w13_base, w2_base, ws=None, out=None,
+                       num_rows: int | None = None):
+    """moe_grouped_ffn with 4-bit experts: w13_base uint8 [P, moe_w4_expert_bytes(2I, H)], w2_base uint8 [P, moe_w4_expert_bytes(H, I)],
+    or raw device pointers (pool views); x bfloat16."""
+    if x.dtype != torch.bfloat16:
+        raise TypeError(f"token rows of 4-bit experts are bfloat16, not {x.dtype}")
+    rows, H = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
+    _need("w13_base", w13_base, torch.uint8, P * moe_w4_expert_bytes(2 * I, H), x)
+    _need("w2_base", w2_base, torch.uint8, P * moe_w4_expert_bytes(H, I), x)
+    y = _result("out", out, (rows, H), x.dtype, x)
+    ws = _scratch(ws, lib().moe_grouped_ffn_w4_workspace_bytes(rows, I), x)
+    _check(lib().moe_grouped_ffn_w4(_ptr(x), rows, k, H, I, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row), _ptr(w13_base), _ptr(w2_base),
+                                    _ptr(y), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
+    return y

@@ -1,0 +1,216 @@
+// Gradients of the grouped SwiGLU expert FFN and of the weighted combine.
+//
+// FFN, for the rows of one slot (g = W1g x, u = W1u x, s = sigmoid(g), a = g s u, y = W2 a):
+//     da  = W2^T dy                     dW2  = sum_r dy a^T
+//     dg  = da u s (1 + g (1 - s))      du   = da g s
+//     dx  = W1g^T dg + W1u^T du         dW13 = sum_r [dg; du] x^T
+// g and u are computed again: kept from the forward pass they would be 2 I values a row for as long as the layers behind this one run.
+#include "grouped_gemm.h"
+
+namespace ew {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void load(const float* p, float* v) {
+    const f32x4 a = *(const f32x4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i];
+  }
+  static __device__ __forceinline__ void store(float* p, const float* v) {
+    f32x4 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = v[i];
+    *(f32x4*)p = a;
+  }
+  static __device__ __forceinline__ float get(float v) { return v; }
+  static __device__ __forceinline__ float put(float v) { return v; }
+};
+template <>
+struct Vec<uint16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void load(const uint16_t* p, float* v) {
+    const u32x4 a = *(const u32x4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(a[i] << 16); v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u); }
+  }
+  static __device__ __forceinline__ uint16_t put(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+  static __device__ __forceinline__ float get(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+  static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
+    u32x4 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = (uint32_t)put(v[2 * i]) | (uint32_t)put(v[2 * i + 1]) << 16;
+    *(u32x4*)p = a;
+  }
+};
+
+// h = [g, u] of a row -> [dg, du] in its place, act -> a; da comes in act.  V: all pointers and I allow wide accesses.
+template <typename T, bool V>
+__global__ __launch_bounds__(256) void k_swiglu_back(const int32_t* __restrict__ offsets, int P, int rows, int I, T* __restrict__ h, T* __restrict__ act) {
+  constexpr int W = V ? Vec<T>::N : 1;
+  const long long n = (long long)min(rows, offsets[P]) * (I / W);
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+    const long long r = i / (I / W);
+    const int c = (int)(i - r * (I / W)) * W;
+    T *pg = h + r * 2 * I + c, *pu = pg + I, *pa = act + r * I + c;
+    float g[W], u[W], d[W];
+    if constexpr (V) { Vec<T>::load(pg, g); Vec<T>::load(pu, u); Vec<T>::load(pa, d); }
+    else { g[0] = Vec<T>::get(*pg); u[0] = Vec<T>::get(*pu); d[0] = Vec<T>::get(*pa); }
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      const float s = 1.f / (1.f + expf(-g[j])), gs = g[j] * s, a = gs * u[j], dg = d[j] * u[j] * s * (1.f + g[j] * (1.f - s));
+      u[j] = d[j] * gs; g[j] = dg; d[j] = a;
+    }
+    if constexpr (V) { Vec<T>::store(pg, g); Vec<T>::store(pu, u); Vec<T>::store(pa, d); }
+    else { *pg = Vec<T>::put(g[0]); *pu = Vec<T>::put(u[0]); *pa = Vec<T>::put(d[0]); }
+  }
+}
+
+// dy[row_of_pair[p]] = w[p] dout[t], dw[p] = <dout[t], y[row_of_pair[p]]>, p = t k + j.  One wave per pair; a token's waves are
+// neighbours, so its row of dout comes from L2 after the first.
+template <typename T, bool V>
+__global__ __launch_bounds__(256) void k_unpermute_back(const T* __restrict__ dout, const T* __restrict__ y, const int32_t* __restrict__ rop,
+                                                        const float* __restrict__ w, long long pairs, int k, int H, T* __restrict__ dy,
+                                                        float* __restrict__ dw) {
+  constexpr int W = V ? Vec<T>::N : 1;
+  const long long p = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (p >= pairs) return;
+  const int lane = threadIdx.x & 63;
+  const T* d = dout + (size_t)(p / k) * H;
+  const size_t row = (size_t)rop[p] * H;
+  const float wp = w[p];
+  float sum = 0.f;
+  for (int h = lane * W; h < H; h += 64 * W) {
+    float v[W], o[W], f[W];
+    if constexpr (V) Vec<T>::load(d + h, v); else v[0] = Vec<T>::get(d[h]);
+    if (y) {
+      if constexpr (V) Vec<T>::load(y + row + h, f); else f[0] = Vec<T>::get(y[row + h]);
+#pragma unroll
+      for (int j = 0; j < W; ++j) sum = fmaf(v[j], f[j], sum);
+    }
+#pragma unroll
+    for (int j = 0; j < W; ++j) o[j] = wp * v[j];
+    if constexpr (V) Vec<T>::store(dy + row + h, o); else dy[row + h] = Vec<T>::put(o[0]);
+  }
+  if (!y) return;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (lane == 0) dw[p] = sum;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+template <typename T>
+int unpermute_back(const T* dout, const T* y, const int32_t* rop, const float* w, long long pairs, int k, int H, T* dy, float* dw, hipStream_t st) {
+  const dim3 grid((unsigned)((pairs + 3) / 4));
+  if (H % Vec<T>::N == 0 && aligned16(dout) && aligned16(y) && aligned16(dy))
+    hipLaunchKernelGGL((k_unpermute_back<T, true>), grid, dim3(256), 0, st, dout, y, rop, w, pairs, k, H, dy, dw);
+  else
+    hipLaunchKernelGGL((k_unpermute_back<T, false>), grid, dim3(256), 0, st, dout, y, rop, w, pairs, k, H, dy, dw);
+  EW_LAUNCH_CHECK("k_unpermute_back");
+  return EW_OK;
+}
+
+template <typename T>
+int swiglu_back(const int32_t* offsets, int P, int rows, int I, T* h, T* act, hipStream_t st) {
+  const bool v = I % Vec<T>::N == 0;
+  const long long n = (long long)rows * (v ? I / Vec<T>::N : I);
+  const dim3 grid((unsigned)(n + 255 < 256ll * 16384 ? (n + 255) / 256 : 16384));
+  if (v) hipLaunchKernelGGL((k_swiglu_back<T, true>), grid, dim3(256), 0, st, offsets, P, rows, I, h, act);
+  else hipLaunchKernelGGL((k_swiglu_back<T, false>), grid, dim3(256), 0, st, offsets, P, rows, I, h, act);
+  EW_LAUNCH_CHECK("k_swiglu_back");
+  return EW_OK;
+}
+
+size_t h_bytes(int num_rows, int I, int dtype) { return align_up((size_t)num_rows * 2 * I * (dtype == EW_BF16 ? 2 : 4), 256); }
+
+}  // namespace
+
+}  // namespace ew
+
+extern "C" size_t moe_grouped_ffn_backward_workspace_bytes(int num_rows, int I, int dtype) {
+  if (num_rows < 1 || I < 1 || (dtype != EW_F32 && dtype != EW_BF16)) return 0;
+  return ew::h_bytes(num_rows, I, dtype) + ew::align_up((size_t)num_rows * I * (dtype == EW_BF16 ? 2 : 4), 256);
+}
+
+extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype, int num_rows, int k, int H, int I, int P, const int32_t* counts,
+                                        const int32_t* offsets, const int32_t* pair_of_row, const void* w13_base, const void* w2_base,
+                                        void* dx_sorted, int first_slot, int num_slots, int dw_dtype, int accumulate, void* dw13, void* dw2,
+                                        void* ws, size_t ws_bytes, void* stream) {
+  using ew::fail;
+  const char* who = "moe_grouped_ffn_backward";
+  if (H < 1 || I < 1 || I > (1 << 30)) return fail(EW_ERR_INVALID_ARG, "%s: need H>=1, 1<=I<=2^30 (got %d, %d)", who, H, I);
+  if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
+  if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
+    return fail(EW_ERR_INVALID_ARG, "%s: weight gradients are float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);
+  if (accumulate && dw_dtype != EW_F32) return fail(EW_ERR_UNSUPPORTED, "%s: only float32 gradients accumulate", who);
+  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (first_slot < 0 || num_slots < 0 || first_slot > P - num_slots)
+    return fail(EW_ERR_INVALID_ARG, "%s: slots [%d, %d + %d) outside 0..P=%d", who, first_slot, first_slot, num_slots, P);
+  const bool want_w = num_slots > 0 && (dw13 || dw2);
+  if (num_rows > 0) {
+    if (!x || !dy || !w13_base || !w2_base) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
+    const size_t need = moe_grouped_ffn_backward_workspace_bytes(num_rows, I, dtype);
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
+      return fail(EW_ERR_WORKSPACE, "%s: workspace needs %zu bytes aligned to 256 (got %zu at %p)", who, need, ws_bytes, ws);
+  }
+  if (!dx_sorted && !want_w) return EW_OK;
+  const hipStream_t st = (hipStream_t)stream;
+  const bool bf16 = dtype == EW_BF16;
+  const int wt = bf16 ? ew::kWBf16 : ew::kWF32;
+  const size_t el = bf16 ? 2 : 4;
+  void *h = ws, *act = (char*)ws + ew::h_bytes(num_rows, I, dtype);
+  ew::GemmArgs a{};
+  int rc;
+  if (num_rows > 0) {
+    a.g = {counts, offsets, pair_of_row, P, num_rows, k};
+    a.x = x; a.w = w13_base; a.out = h; a.K = H; a.N = 2 * I; a.slot_bytes = (size_t)2 * I * H * el;
+    if ((rc = ew::launch_gemm(ew::kFwd, wt, bf16, !bf16, a, st))) return rc;
+    a.g.por = nullptr; a.g.k = 1;  // from here on the sorted rows themselves
+    a.x = dy; a.w = w2_base; a.out = act; a.K = H; a.N = I; a.slot_bytes = (size_t)I * H * el;
+    if ((rc = ew::launch_gemm(ew::kDgrad, wt, bf16, !bf16, a, st))) return rc;
+    rc = bf16 ? ew::swiglu_back(offsets, P, num_rows, I, (uint16_t*)h, (uint16_t*)act, st) : ew::swiglu_back(offsets, P, num_rows, I, (float*)h, (float*)act, st);
+    if (rc) return rc;
+    if (dx_sorted) {
+      a.x = h; a.w = w13_base; a.out = dx_sorted; a.K = 2 * I; a.N = H; a.slot_bytes = (size_t)2 * I * H * el;
+      if ((rc = ew::launch_gemm(ew::kDgrad, wt, bf16, !bf16, a, st))) return rc;
+    }
+  }
+  if (!want_w) return EW_OK;
+  a.first_slot = first_slot; a.num_slots = num_slots; a.accumulate = accumulate != 0;
+  if (dw13) {
+    a.g = {counts, offsets, pair_of_row, P, num_rows, k};
+    a.x = x; a.w = h; a.out = dw13; a.K = H; a.N = 2 * I;
+    if ((rc = ew::launch_gemm(ew::kWgrad, wt, bf16, dw_dtype == EW_F32, a, st))) return rc;
+  }
+  if (dw2) {
+    a.g = {counts, offsets, nullptr, P, num_rows, 1};
+    a.x = act; a.w = dy; a.out = dw2; a.K = I; a.N = H;
+    if ((rc = ew::launch_gemm(ew::kWgrad, wt, bf16, dw_dtype == EW_F32, a, st))) return rc;
+  }
+  return EW_OK;
+}
+
+extern "C" int moe_unpermute_backward(const void* dout, const void* y_sorted, const int32_t* row_of_pair, const float* topk_w, int T, int k, int H,
+                                      int dtype, void* dy_sorted, float* dw, void* stream) {
+  using ew::fail;
+  const char* who = "moe_unpermute_backward";
+  if (T < 0 || k < 1 || H < 1) return fail(EW_ERR_INVALID_ARG, "%s: need T>=0, k>=1, H>=1 (got %d, %d, %d)", who, T, k, H);
+  if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
+  if ((long long)T * k >= (1ll << 31)) return fail(EW_ERR_UNSUPPORTED, "%s: the row count must be below 2^31", who);
+  if (T == 0) return EW_OK;
+  if (!dout || !row_of_pair || !topk_w || !dy_sorted || !y_sorted != !dw)
+    return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer (y_sorted and dw: both or neither)", who);
+  const long long pairs = (long long)T * k;
+  const hipStream_t st = (hipStream_t)stream;
+  if (dtype == EW_BF16)
+    return ew::unpermute_back((const uint16_t*)dout, (const uint16_t*)y_sorted, row_of_pair, topk_w, pairs, k, H, (uint16_t*)dy_sorted, dw, st);
+  return ew::unpermute_back((const float*)dout, (const float*)y_sorted, row_of_pair, topk_w, pairs, k, H, (float*)dy_sorted, dw, st);
+}

@@ -1,0 +1,199 @@
+// Matrix products grouped by expert over ragged rows, in three directions (forward, input gradient, weight gradient).
+//
+// k_gemm_any is the kernel for fp32, and for bf16 and 4-bit sizes that the matrix-core kernels do not take: plain fp32 products
+// and sums on v_mfma_f32_32x32x2_f32 whatever the inputs' type, any sizes, any alignment.  A workgroup makes 64 x 64 outputs, its four
+// waves 32 x 32 each; 16 contraction steps at a time reach LDS contraction-major, so that both operands are read without bank
+// conflicts whichever way they lie in memory.  Outputs of a lane are four neighbours along the contiguous axis.
+#include "grouped_gemm.h"
+
+namespace ew {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ float as_f32(float v) { return v; }
+__device__ __forceinline__ float as_f32(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+
+// E2M1 value times 2^(scale - 127); scale 255 means NaN.
+__device__ __forceinline__ float w4_value(uint32_t code, uint32_t scale) {
+  const uint32_t e = code >> 1 & 3, m = code & 1;
+  const float mag = e ? __uint_as_float((126 + e) << 23 | m << 22) : 0.5f * (float)m;
+  const float v = ldexpf(code & 8 ? -mag : mag, (int)scale - 127);
+  return scale == 255 ? __uint_as_float(0x7FC00000u) : v;
+}
+
+constexpr int kTile = 64, kStep = 16, kPitch = kTile + 4;
+
+// Four elements of an operand, fp32: element (o + i, kk) for i < 4 where ALONG_O, otherwise (o, kk + i).
+// TW: type of the elements; float, uint16_t (bf16), or uint8_t for a 4-bit expert's bytes.
+template <int WAY, typename TX, typename TW>
+__global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n, int out_f32) {
+  __shared__ float s_a[kStep][kPitch], s_b[kStep][kPitch];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tile = blockIdx.x % tiles_n, unit = blockIdx.x / tiles_n;
+  const int K = a.K, N = a.N;
+  RowChunk ch;
+  int na, nb, a0, b0, len;  // extents and start of the output tile along A (contiguous) and B, length of the contraction
+  if constexpr (WAY == kWgrad) {
+    const int slot = a.first_slot + unit;
+    const int off = a.g.offsets[slot];
+    ch = {slot, off, max(0, min(a.g.counts[slot], a.g.rows - off))};
+    const int tk = (K + kTile - 1) / kTile;
+    a0 = tile % tk * kTile; b0 = tile / tk * kTile;
+    na = K; nb = N; len = ch.rows;
+    if (len == 0 && a.accumulate) return;
+  } else {
+    ch = find_chunk<kTile, 1>(a.g, unit);
+    if (ch.slot < 0) return;
+    a0 = tile * kTile; b0 = 0;
+    na = N; nb = ch.rows; len = K;
+  }
+  const TX* x = (const TX*)a.x;
+  const unsigned char* ws = (const unsigned char*)a.w + (WAY == kWgrad ? 0 : (size_t)ch.slot * a.slot_bytes);
+  // operand A: weights, or x of the weight gradient; operand B: token rows, or dy
+  auto at_a = [&](int o, int kk) -> float {  // o < na, kk < len
+    if constexpr (WAY == kWgrad) return as_f32(x[(size_t)source_row(a.g, ch.first + kk) * K + o]);
+    else if constexpr (sizeof(TW) == 1) {
+      const uint32_t two = ws[(size_t)o * (K / 2) + kk / 2];
+      return w4_value(kk & 1 ? two >> 4 : two & 15, ws[w4_scales_at(N, K) + (size_t)o * (K / 32) + kk / 32]);
+    } else return as_f32(((const TW*)ws)[WAY == kFwd ? (size_t)o * K + kk : (size_t)kk * N + o]);
+  };
+  const int row_k = tid >> 2, k_k = (tid & 3) * 4;   // a thread's four elements along the contraction
+  const int k_o = tid >> 4, row_o = (tid & 15) * 4;  // and across it
+  int src = 0;
+  if constexpr (WAY != kWgrad) src = row_k < nb ? source_row(a.g, ch.first + row_k) : 0;
+  f32x16 acc = {};
+  for (int k0 = 0; k0 < len; k0 += kStep) {
+    float va[4], vb[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (WAY == kFwd) {
+        const int o = a0 + row_k, kk = k0 + k_k + i;
+        va[i] = o < na && kk < len ? at_a(o, kk) : 0.f;
+      } else {
+        const int o = a0 + row_o + i, kk = k0 + k_o;
+        va[i] = o < na && kk < len ? at_a(o, kk) : 0.f;
+      }
+      if constexpr (WAY == kWgrad) {
+        const int o = b0 + row_o + i, kk = k0 + k_o;
+        vb[i] = o < nb && kk < len ? as_f32(((const TW*)ws)[(size_t)(ch.first + kk) * N + o]) : 0.f;
+      } else {
+        const int kk = k0 + k_k + i;
+        vb[i] = row_k < nb && kk < len ? as_f32(x[(size_t)src * K + kk]) : 0.f;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (WAY == kFwd) s_a[k_k + i][row_k] = va[i]; else s_a[k_o][row_o + i] = va[i];
+      if constexpr (WAY == kWgrad) s_b[k_o][row_o + i] = vb[i]; else s_b[k_k + i][row_k] = vb[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kStep; j += 2)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(s_a[j + (lane >> 5)][(wave & 1) * 32 + (lane & 31)],
+                                                 s_b[j + (lane >> 5)][(wave >> 1) * 32 + (lane & 31)], acc, 0, 0, 0);
+  }
+  // lane l: B element l % 32, A elements 8 (i / 4) + 4 (l / 32) + i % 4
+  const int b = b0 + (wave >> 1) * 32 + (lane & 31);
+  if (b >= nb) return;
+  const size_t at = WAY == kWgrad ? ((size_t)unit * N + b) * K : (size_t)(ch.first + b) * N;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int o = a0 + (wave & 1) * 32 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+    if (o >= na) continue;
+    if (out_f32) {
+      float* p = (float*)a.out + at + o;
+      put(p, WAY == kWgrad && a.accumulate ? *p + acc[i] : acc[i]);
+    } else {
+      put((uint16_t*)a.out + at + o, acc[i]);
+    }
+  }
+}
+
+template <int WAY, typename TX, typename TW>
+int launch_any(const GemmArgs& a, bool out_f32, hipStream_t st) {
+  long long units, tiles;
+  if (WAY == kWgrad) {
+    units = a.num_slots;
+    tiles = (long long)ceil_div(a.K, kTile) * ceil_div(a.N, kTile);
+  } else {
+    units = max_chunks(a.g.rows, a.g.P, kTile);
+    tiles = ceil_div(a.N, kTile);
+  }
+  if (units * tiles >= (1ll << 31)) return fail(EW_ERR_UNSUPPORTED, "grouped product: too many output tiles for one launch");
+  if (units * tiles == 0) return EW_OK;
+  hipLaunchKernelGGL((k_gemm_any<WAY, TX, TW>), dim3((unsigned)(units * tiles)), dim3(256), 0, st, a, (int)tiles, (int)out_f32);
+  EW_LAUNCH_CHECK("k_gemm_any");
+  return EW_OK;
+}
+
+}  // namespace
+
+int launch_gemm_any(int way, int weights, bool bf16_rows, bool out_f32, const GemmArgs& a, hipStream_t st) {
+  if (weights == kW4) return launch_any<kFwd, uint16_t, uint8_t>(a, out_f32, st);
+  if (bf16_rows) {
+    if (way == kFwd) return launch_any<kFwd, uint16_t, uint16_t>(a, out_f32, st);
+    if (way == kDgrad) return launch_any<kDgrad, uint16_t, uint16_t>(a, out_f32, st);
+    return launch_any<kWgrad, uint16_t, uint16_t>(a, out_f32, st);
+  }
+  if (way == kFwd) return launch_any<kFwd, float, float>(a, out_f32, st);
+  if (way == kDgrad) return launch_any<kDgrad, float, float>(a, out_f32, st);
+  return launch_any<kWgrad, float, float>(a, out_f32, st);
+}
+
+int launch_gemm(int way, int weights, bool bf16_rows, bool out_f32, const GemmArgs& a, hipStream_t st) {
+  return launch_gemm_any(way, weights, bf16_rows, out_f32, a, st);
+}
+
+int check_rows(const char* who, int num_rows, int k, int P, const void* counts, const void* offsets) {
+  if (num_rows < 0 || k < 1 || P < 1) return fail(EW_ERR_INVALID_ARG, "%s: need num_rows>=0, k>=1, P>=1 (got %d, %d, %d)", who, num_rows, k, P);
+  if (!counts || !offsets) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
+  return EW_OK;
+}
+
+}  // namespace ew
+
+extern "C" int moe_grouped_gemm(const void* x, int dtype, int num_rows, int k, int K, int N, int P, int transposed,
+                                const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row, const void* w_base, void* y,
+                                void* stream) {
+  using ew::fail;
+  const char* who = "moe_grouped_gemm";
+  if (K < 1 || N < 1) return fail(EW_ERR_INVALID_ARG, "%s: need K>=1, N>=1 (got %d, %d)", who, K, N);
+  if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
+  if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
+  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (!x || !w_base || !y) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
+  ew::GemmArgs a{};
+  a.g = {counts, offsets, pair_of_row, P, num_rows, k};
+  a.x = x; a.w = w_base; a.out = y; a.K = K; a.N = N;
+  a.slot_bytes = (size_t)N * K * (dtype == EW_BF16 ? 2 : 4);
+  return ew::launch_gemm(transposed ? ew::kDgrad : ew::kFwd, dtype == EW_BF16 ? ew::kWBf16 : ew::kWF32, dtype == EW_BF16, dtype == EW_F32, a,
+                         (hipStream_t)stream);
+}
+
+extern "C" int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_rows, int k, int K, int N, int P,
+                                      const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row, int first_slot,
+                                      int num_slots, int dw_dtype, int accumulate, void* dw, void* stream) {
+  using ew::fail;
+  const char* who = "moe_grouped_gemm_wgrad";
+  if (K < 1 || N < 1) return fail(EW_ERR_INVALID_ARG, "%s: need K>=1, N>=1 (got %d, %d)", who, K, N);
+  if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
+  if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
+    return fail(EW_ERR_INVALID_ARG, "%s: dw is float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);
+  if (accumulate && dw_dtype != EW_F32) return fail(EW_ERR_UNSUPPORTED, "%s: only float32 gradients accumulate", who);
+  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (first_slot < 0 || num_slots < 0 || first_slot > P - num_slots)
+    return fail(EW_ERR_INVALID_ARG, "%s: slots [%d, %d + %d) outside 0..P=%d", who, first_slot, first_slot, num_slots, P);
+  if (num_slots == 0) return EW_OK;
+  if (!dw || (num_rows > 0 && (!dy || !x))) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
+  ew::GemmArgs a{};
+  a.g = {counts, offsets, pair_of_row, P, num_rows, k};
+  a.x = x; a.w = dy; a.out = dw; a.K = K; a.N = N;
+  a.first_slot = first_slot; a.num_slots = num_slots; a.accumulate = accumulate != 0;
+  return ew::launch_gemm(ew::kWgrad, dtype == EW_BF16 ? ew::kWBf16 : ew::kWF32, dtype == EW_BF16, dw_dtype == EW_F32, a, (hipStream_t)stream);
+}
