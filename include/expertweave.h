@@ -403,7 +403,7 @@ int moe_layer_forward(const ew_layer* layer, const void* x, const int32_t* adapt
  * All of them take rows as the permutation leaves them: sorted by slot, slot s with counts[s] rows from row
  * offsets[s] on, row r made from pair pair_of_row[r] (NULL: pair r), that is from token pair / k.
  * num_rows is the room that the row arrays have; offsets[P] <= num_rows rows exist, and rows behind the last
- * one are neither read nor written.  A slot without rows is never dereferenced.  Nothing is kept between
+ * one are neither read nor written.  x has num_tokens rows.  A slot without rows is never dereferenced.  Nothing is kept between
  * calls and no call needs scratch of its own unless it takes a workspace; results do not depend on the
  * launch (no atomics), so calls repeat bit for bit, also out of a captured graph.
  * ===================================================================================== */
@@ -413,24 +413,24 @@ int moe_layer_forward(const ew_layer* layer, const void* x, const int32_t* adapt
  *   transposed != 0:  y[r][n] = sum_k x[t][k] * w_base[s][k][n],   w_base [P, K, N]
  * with t = pair_of_row[r] / k.  The second form is the input gradient of the first: dx = dy W takes
  * x = dy (sorted rows: pair_of_row NULL, k = 1), K = the forward product's N and N = its K.
- *   x [dev] dtype [*, K]; y [dev] dtype [num_rows, N]
+ *   x [dev] dtype [num_tokens, K]; y [dev] dtype [num_rows, N]
  * fp32 accumulation, rounded once into y.  Any K and N; bf16 runs on the bf16 matrix cores where K and N are
  * multiples of 8, x, w_base and y are aligned to 16 bytes and a slot's weights and the rows of x are
  * addressable with 32-bit byte offsets, and in fp32 otherwise.
  * num_rows = 0 is a no-op.  Errors: INVALID_ARG, UNSUPPORTED (a launch of 2^31 workgroups), HIP. */
-int moe_grouped_gemm(const void* x, int dtype, int num_rows, int k, int K, int N, int P, int transposed,
-                     const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
+int moe_grouped_gemm(const void* x, int dtype, int num_tokens, int num_rows, int k, int K, int N, int P,
+                     int transposed, const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
                      const void* w_base, void* y, void* stream);
 
 /* Weight gradients of moe_grouped_gemm (transposed == 0) for slots first_slot .. first_slot+num_slots-1:
  *   dw[s - first_slot][n][k] (+)= sum over the rows r of slot s of dy[r][n] * x[pair_of_row[r] / k][k]
- *   dy [dev] dtype [num_rows, N]; x [dev] dtype [*, K]
+ *   dy [dev] dtype [num_rows, N]; x [dev] dtype [num_tokens, K]
  *   dw [dev] dw_dtype [num_slots, N, K]: EW_F32, or EW_BF16 for bf16 rows (rounded once).  accumulate != 0
  *      adds to what dw holds (EW_F32 only); otherwise slots without rows get zeros.
  * A product w of the second form (transposed != 0) has the same gradient with dy and x exchanged.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
-int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_rows, int k, int K, int N, int P,
-                           const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
+int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_tokens, int num_rows, int k, int K,
+                           int N, int P, const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
                            int first_slot, int num_slots, int dw_dtype, int accumulate, void* dw,
                            void* stream);
 
@@ -438,17 +438,17 @@ int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_row
  * first_slot .. first_slot+num_slots-1 (an adapter's slots, or all).  With g = W1g x, u = W1u x, s = sigmoid(g):
  *   da = W2^T dy, dg = da u s (1 + g (1 - s)), du = da g s, a = g s u
  *   dx_sorted[r] = W1g^T dg + W1u^T du;  dw13 (+)= sum_r [dg; du] x^T;  dw2 (+)= sum_r dy a^T
- *   x [dev] dtype [*, H]; dy [dev] dtype [num_rows, H]; w13_base, w2_base as for moe_grouped_ffn
+ *   x [dev] dtype [num_tokens, H]; dy [dev] dtype [num_rows, H]; w13_base, w2_base as for moe_grouped_ffn
  *   dx_sorted [dev] dtype [num_rows, H], one row per pair, or NULL.  A token's input gradient is the sum over its
  *      pairs: moe_unpermute(dx_sorted, row_of_pair, ones).
  *   dw13 [dev] dw_dtype [num_slots, 2I, H], dw2 [dev] dw_dtype [num_slots, H, I], either may be NULL;
  *      dw_dtype and accumulate as for moe_grouped_gemm_wgrad
- * g and u are computed again.  bf16: g, u, da, dg, du and a are bf16 between the products.
+ * g and u are computed again.  bf16: dg, du and a are rounded to bf16 between the products, nothing else is.
  * Any H and I (what runs on the bf16 matrix cores: as moe_grouped_gemm).
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
 size_t moe_grouped_ffn_backward_workspace_bytes(int num_rows, int I, int dtype);
-int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype, int num_rows, int k, int H, int I, int P,
-                             const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
+int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype, int num_tokens, int num_rows, int k, int H,
+                             int I, int P, const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
                              const void* w13_base, const void* w2_base, void* dx_sorted, int first_slot,
                              int num_slots, int dw_dtype, int accumulate, void* dw13, void* dw2, void* ws,
                              size_t ws_bytes, void* stream);
@@ -487,12 +487,12 @@ int moe_dequantize_w4(const void* w4, int dtype, int num_experts, int N, int K, 
  * Limits: sizes that can be packed.  Fast where K is a multiple of 128 and N of 16 (the FFN: H and I of 128) and
  * pointers are aligned to 16 bytes; plain otherwise.
  * num_rows = 0 is a no-op.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
-int moe_grouped_gemm_w4(const void* x, int num_rows, int k, int K, int N, int P, const int32_t* counts,
-                        const int32_t* offsets, const int32_t* pair_of_row, const void* w4_base, void* y,
+int moe_grouped_gemm_w4(const void* x, int num_tokens, int num_rows, int k, int K, int N, int P,
+                        const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row, const void* w4_base, void* y,
                         void* stream);
 size_t moe_grouped_ffn_w4_workspace_bytes(int num_rows, int I);
-int moe_grouped_ffn_w4(const void* x, int num_rows, int k, int H, int I, int P, const int32_t* counts,
-                       const int32_t* offsets, const int32_t* pair_of_row, const void* w13_base,
+int moe_grouped_ffn_w4(const void* x, int num_tokens, int num_rows, int k, int H, int I, int P,
+                       const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row, const void* w13_base,
                        const void* w2_base, void* y_sorted, void* ws, size_t ws_bytes, void* stream);
 
 /* ===================================================================================== *

@@ -58,17 +58,17 @@ SIGNATURES = {
     "moe_layer_forward": (_int, [_vp, _vp, _vp, _int, _vp, _vp, _vp, _vp, C.c_float, _vp]),
     "moe_gate_logits": (_int, [_vp, _int, _vp, _int, _int, _int, _vp, _vp, _vp, _vp]),
     "moe_rmsnorm": (_int, [_vp, _int, _int, _int, C.c_float, _vp, _vp]),
-    "moe_grouped_gemm": (_int, [_vp] + [_int] * 7 + [_vp] * 6),
-    "moe_grouped_gemm_wgrad": (_int, [_vp, _vp] + [_int] * 6 + [_vp] * 3 + [_int] * 4 + [_vp] * 2),
+    "moe_grouped_gemm": (_int, [_vp] + [_int] * 8 + [_vp] * 6),
+    "moe_grouped_gemm_wgrad": (_int, [_vp, _vp] + [_int] * 7 + [_vp] * 3 + [_int] * 4 + [_vp] * 2),
     "moe_grouped_ffn_backward_workspace_bytes": (_sz, [_int, _int, _int]),
-    "moe_grouped_ffn_backward": (_int, [_vp, _vp] + [_int] * 6 + [_vp] * 6 + [_int] * 4 + [_vp] * 3 + [_sz, _vp]),
+    "moe_grouped_ffn_backward": (_int, [_vp, _vp] + [_int] * 7 + [_vp] * 6 + [_int] * 4 + [_vp] * 3 + [_sz, _vp]),
     "moe_unpermute_backward": (_int, [_vp] * 4 + [_int] * 4 + [_vp] * 3),
     "moe_w4_expert_bytes": (_sz, [_int, _int]),
     "moe_quantize_w4": (_int, [_vp] + [_int] * 4 + [_vp] * 2),
     "moe_dequantize_w4": (_int, [_vp] + [_int] * 4 + [_vp] * 2),
-    "moe_grouped_gemm_w4": (_int, [_vp] + [_int] * 5 + [_vp] * 6),
+    "moe_grouped_gemm_w4": (_int, [_vp] + [_int] * 6 + [_vp] * 6),
     "moe_grouped_ffn_w4_workspace_bytes": (_sz, [_int, _int]),
-    "moe_grouped_ffn_w4": (_int, [_vp] + [_int] * 5 + [_vp] * 7 + [_sz, _vp]),
+    "moe_grouped_ffn_w4": (_int, [_vp] + [_int] * 6 + [_vp] * 7 + [_sz, _vp]),
     "ew_probe_stream": (_int, [_vp, _vp, _sz, _int, _vp]),
     "ew_probe_mfma_bf16": (_int, [_int, _int, _int, _vp, _vp]),
     "ew_tune_ffn": (None, [_int, _int, _int, _int, _int, _int, _int]),
@@ -461,7 +461,7 @@ def moe_grouped_gemm(x, k: int, N: int, P: int, counts, offsets, pair_of_row, w_
     rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
     _need("w_base", w_base, x.dtype, P * N * K, x)
     y = _result("out", out, (rows, N), x.dtype, x)
-    _check(lib().moe_grouped_gemm(_ptr(x), _dtype_code(x), rows, k, K, N, P, int(transposed), _ptr(counts), _ptr(offsets),
+    _check(lib().moe_grouped_gemm(_ptr(x), _dtype_code(x), x.shape[0], rows, k, K, N, P, int(transposed), _ptr(counts), _ptr(offsets),
                                   _ptr(pair_of_row), _ptr(w_base), _ptr(y), _stream()))
     return y
 
@@ -477,7 +477,7 @@ def moe_grouped_gemm_wgrad(dy, x, k: int, P: int, counts, offsets, pair_of_row, 
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     dw = _result("out", out, (max(n, 0), N, K), dtype, x)
-    _check(lib().moe_grouped_gemm_wgrad(_ptr(dy), _ptr(x), _dtype_code(x), rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
+    _check(lib().moe_grouped_gemm_wgrad(_ptr(dy), _ptr(x), _dtype_code(x), x.shape[0], rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
                                         first_slot, n, _dtype_code(dw), int(accumulate), _ptr(dw), _stream()))
     return dw
 
@@ -503,7 +503,7 @@ def moe_grouped_ffn_backward(x, dy, k: int, I: int, P: int, counts, offsets, pai
     else:
         dw13 = dw2 = None
     ws = _scratch(ws, lib().moe_grouped_ffn_backward_workspace_bytes(rows, I, _dtype_code(x)), x)
-    _check(lib().moe_grouped_ffn_backward(_ptr(x), _ptr(dy), _dtype_code(x), rows, k, H, I, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
+    _check(lib().moe_grouped_ffn_backward(_ptr(x), _ptr(dy), _dtype_code(x), x.shape[0], rows, k, H, I, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
                                           _ptr(w13_base), _ptr(w2_base), _ptr(dx), first_slot, n, EW_F32 if dw_dtype == torch.float32 else EW_BF16,
                                           int(accumulate), _ptr(dw13), _ptr(dw2), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
     return dx, dw13, dw2
@@ -564,7 +564,7 @@ def moe_grouped_gemm_w4(x, k: int, N: int, P: int, counts, offsets, pair_of_row,
     rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
     _need("w4_base", w4_base, torch.uint8, P * moe_w4_expert_bytes(N, K), x)
     y = _result("out", out, (rows, N), x.dtype, x)
-    _check(lib().moe_grouped_gemm_w4(_ptr(x), rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row), _ptr(w4_base), _ptr(y), _stream()))
+    _check(lib().moe_grouped_gemm_w4(_ptr(x), x.shape[0], rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row), _ptr(w4_base), _ptr(y), _stream()))
     return y
 
 
@@ -579,6 +579,6 @@ def moe_grouped_ffn_w4(x, k: int, I: int, P: int, counts, offsets, pair_of_row, 
     _need("w2_base", w2_base, torch.uint8, P * moe_w4_expert_bytes(H, I), x)
     y = _result("out", out, (rows, H), x.dtype, x)
     ws = _scratch(ws, lib().moe_grouped_ffn_w4_workspace_bytes(rows, I), x)
-    _check(lib().moe_grouped_ffn_w4(_ptr(x), rows, k, H, I, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row), _ptr(w13_base), _ptr(w2_base),
+    _check(lib().moe_grouped_ffn_w4(_ptr(x), x.shape[0], rows, k, H, I, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row), _ptr(w13_base), _ptr(w2_base),
                                     _ptr(y), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
     return y

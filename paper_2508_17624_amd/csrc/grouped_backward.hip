@@ -5,6 +5,9 @@
 //     dg  = da u s (1 + g (1 - s))      du   = da g s
 //     dx  = W1g^T dg + W1u^T du         dW13 = sum_r [dg; du] x^T
 // g and u are computed again: kept from the forward pass they would be 2 I values a row for as long as the layers behind this one run.
+// They stay in fp32 until dg and du are formed, in the epilogue of the product that makes da: of what lies between the products only
+// dg, du and a are rounded to bf16, as operands of the matrix cores.  (With g, u and da in bf16 too the gradients' relative error is 3.5e-3
+// instead of 2.4e-3.)
 #include "grouped_gemm.h"
 
 namespace ew {
@@ -51,28 +54,6 @@ struct Vec<uint16_t> {
   }
 };
 
-// h = [g, u] of a row -> [dg, du] in its place, act -> a; da comes in act.  V: all pointers and I allow wide accesses.
-template <typename T, bool V>
-__global__ __launch_bounds__(256) void k_swiglu_back(const int32_t* __restrict__ offsets, int P, int rows, int I, T* __restrict__ h, T* __restrict__ act) {
-  constexpr int W = V ? Vec<T>::N : 1;
-  const long long n = (long long)min(rows, offsets[P]) * (I / W);
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-    const long long r = i / (I / W);
-    const int c = (int)(i - r * (I / W)) * W;
-    T *pg = h + r * 2 * I + c, *pu = pg + I, *pa = act + r * I + c;
-    float g[W], u[W], d[W];
-    if constexpr (V) { Vec<T>::load(pg, g); Vec<T>::load(pu, u); Vec<T>::load(pa, d); }
-    else { g[0] = Vec<T>::get(*pg); u[0] = Vec<T>::get(*pu); d[0] = Vec<T>::get(*pa); }
-#pragma unroll
-    for (int j = 0; j < W; ++j) {
-      const float s = 1.f / (1.f + expf(-g[j])), gs = g[j] * s, a = gs * u[j], dg = d[j] * u[j] * s * (1.f + g[j] * (1.f - s));
-      u[j] = d[j] * gs; g[j] = dg; d[j] = a;
-    }
-    if constexpr (V) { Vec<T>::store(pg, g); Vec<T>::store(pu, u); Vec<T>::store(pa, d); }
-    else { *pg = Vec<T>::put(g[0]); *pu = Vec<T>::put(u[0]); *pa = Vec<T>::put(d[0]); }
-  }
-}
-
 // dy[row_of_pair[p]] = w[p] dout[t], dw[p] = <dout[t], y[row_of_pair[p]]>, p = t k + j.  One wave per pair; a token's waves are
 // neighbours, so its row of dout comes from L2 after the first.
 template <typename T, bool V>
@@ -118,18 +99,13 @@ int unpermute_back(const T* dout, const T* y, const int32_t* rop, const float* w
   return EW_OK;
 }
 
-template <typename T>
-int swiglu_back(const int32_t* offsets, int P, int rows, int I, T* h, T* act, hipStream_t st) {
-  const bool v = I % Vec<T>::N == 0;
-  const long long n = (long long)rows * (v ? I / Vec<T>::N : I);
-  const dim3 grid((unsigned)(n + 255 < 256ll * 16384 ? (n + 255) / 256 : 16384));
-  if (v) hipLaunchKernelGGL((k_swiglu_back<T, true>), grid, dim3(256), 0, st, offsets, P, rows, I, h, act);
-  else hipLaunchKernelGGL((k_swiglu_back<T, false>), grid, dim3(256), 0, st, offsets, P, rows, I, h, act);
-  EW_LAUNCH_CHECK("k_swiglu_back");
-  return EW_OK;
+// Workspace: g and u [rows, 2I] fp32, dg and du [rows, 2I], a [rows, I].
+struct BackScratch { size_t dh, act, all; };
+BackScratch back_scratch(int num_rows, int I, int dtype) {
+  const size_t el = dtype == EW_BF16 ? 2 : 4, n = (size_t)num_rows * I;
+  const size_t dh = align_up(n * 8, 256), act = dh + align_up(n * 2 * el, 256);
+  return {dh, act, act + align_up(n * el, 256)};
 }
-
-size_t h_bytes(int num_rows, int I, int dtype) { return align_up((size_t)num_rows * 2 * I * (dtype == EW_BF16 ? 2 : 4), 256); }
 
 }  // namespace
 
@@ -137,10 +113,10 @@ size_t h_bytes(int num_rows, int I, int dtype) { return align_up((size_t)num_row
 
 extern "C" size_t moe_grouped_ffn_backward_workspace_bytes(int num_rows, int I, int dtype) {
   if (num_rows < 1 || I < 1 || (dtype != EW_F32 && dtype != EW_BF16)) return 0;
-  return ew::h_bytes(num_rows, I, dtype) + ew::align_up((size_t)num_rows * I * (dtype == EW_BF16 ? 2 : 4), 256);
+  return ew::back_scratch(num_rows, I, dtype).all;
 }
 
-extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype, int num_rows, int k, int H, int I, int P, const int32_t* counts,
+extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype, int num_tokens, int num_rows, int k, int H, int I, int P, const int32_t* counts,
                                         const int32_t* offsets, const int32_t* pair_of_row, const void* w13_base, const void* w2_base,
                                         void* dx_sorted, int first_slot, int num_slots, int dw_dtype, int accumulate, void* dw13, void* dw2,
                                         void* ws, size_t ws_bytes, void* stream) {
@@ -151,7 +127,7 @@ extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype
   if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
     return fail(EW_ERR_INVALID_ARG, "%s: weight gradients are float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);
   if (accumulate && dw_dtype != EW_F32) return fail(EW_ERR_UNSUPPORTED, "%s: only float32 gradients accumulate", who);
-  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
   if (first_slot < 0 || num_slots < 0 || first_slot > P - num_slots)
     return fail(EW_ERR_INVALID_ARG, "%s: slots [%d, %d + %d) outside 0..P=%d", who, first_slot, first_slot, num_slots, P);
   const bool want_w = num_slots > 0 && (dw13 || dw2);
@@ -166,34 +142,33 @@ extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype
   const bool bf16 = dtype == EW_BF16;
   const int wt = bf16 ? ew::kWBf16 : ew::kWF32;
   const size_t el = bf16 ? 2 : 4;
-  void *h = ws, *act = (char*)ws + ew::h_bytes(num_rows, I, dtype);
+  const ew::BackScratch at = ew::back_scratch(num_rows, I, dtype);
+  void *dh = (char*)ws + at.dh, *act = (char*)ws + at.act;
+  const ew::GroupedRows mapped{counts, offsets, pair_of_row, P, num_rows, k}, sorted{counts, offsets, nullptr, P, num_rows, 1};
+  const int ep = bf16 ? ew::kEpBf16 : ew::kEpF32;
   ew::GemmArgs a{};
   int rc;
   if (num_rows > 0) {
-    a.g = {counts, offsets, pair_of_row, P, num_rows, k};
-    a.x = x; a.w = w13_base; a.out = h; a.K = H; a.N = 2 * I; a.slot_bytes = (size_t)2 * I * H * el;
-    if ((rc = ew::launch_gemm(ew::kFwd, wt, bf16, !bf16, a, st))) return rc;
-    a.g.por = nullptr; a.g.k = 1;  // from here on the sorted rows themselves
-    a.x = dy; a.w = w2_base; a.out = act; a.K = H; a.N = I; a.slot_bytes = (size_t)I * H * el;
-    if ((rc = ew::launch_gemm(ew::kDgrad, wt, bf16, !bf16, a, st))) return rc;
-    rc = bf16 ? ew::swiglu_back(offsets, P, num_rows, I, (uint16_t*)h, (uint16_t*)act, st) : ew::swiglu_back(offsets, P, num_rows, I, (float*)h, (float*)act, st);
-    if (rc) return rc;
+    a.g = mapped; a.x = x; a.x_rows = num_tokens; a.w = w13_base; a.out = ws; a.K = H; a.N = 2 * I; a.slot_bytes = (size_t)2 * I * H * el;
+    if ((rc = ew::launch_gemm(ew::kFwd, wt, ew::kEpF32, bf16, a, st))) return rc;
+    a.g = sorted; a.x = dy; a.x_rows = num_rows; a.w = w2_base; a.out = act; a.h = (const float*)ws; a.dh = dh;
+    a.K = H; a.N = I; a.slot_bytes = (size_t)I * H * el;
+    if ((rc = ew::launch_gemm(ew::kDgrad, wt, ew::kEpBack, bf16, a, st))) return rc;
     if (dx_sorted) {
-      a.x = h; a.w = w13_base; a.out = dx_sorted; a.K = 2 * I; a.N = H; a.slot_bytes = (size_t)2 * I * H * el;
-      if ((rc = ew::launch_gemm(ew::kDgrad, wt, bf16, !bf16, a, st))) return rc;
+      a.x = dh; a.w = w13_base; a.out = dx_sorted; a.K = 2 * I; a.N = H; a.slot_bytes = (size_t)2 * I * H * el;
+      if ((rc = ew::launch_gemm(ew::kDgrad, wt, ep, bf16, a, st))) return rc;
     }
   }
   if (!want_w) return EW_OK;
+  const int dw_ep = dw_dtype == EW_F32 ? ew::kEpF32 : ew::kEpBf16;
   a.first_slot = first_slot; a.num_slots = num_slots; a.accumulate = accumulate != 0;
   if (dw13) {
-    a.g = {counts, offsets, pair_of_row, P, num_rows, k};
-    a.x = x; a.w = h; a.out = dw13; a.K = H; a.N = 2 * I;
-    if ((rc = ew::launch_gemm(ew::kWgrad, wt, bf16, dw_dtype == EW_F32, a, st))) return rc;
+    a.g = mapped; a.x = x; a.x_rows = num_tokens; a.w = dh; a.out = dw13; a.K = H; a.N = 2 * I;
+    if ((rc = ew::launch_gemm(ew::kWgrad, wt, dw_ep, bf16, a, st))) return rc;
   }
   if (dw2) {
-    a.g = {counts, offsets, nullptr, P, num_rows, 1};
-    a.x = act; a.w = dy; a.out = dw2; a.K = I; a.N = H;
-    if ((rc = ew::launch_gemm(ew::kWgrad, wt, bf16, dw_dtype == EW_F32, a, st))) return rc;
+    a.g = sorted; a.x = act; a.x_rows = num_rows; a.w = dy; a.out = dw2; a.K = I; a.N = H;
+    if ((rc = ew::launch_gemm(ew::kWgrad, wt, dw_ep, bf16, a, st))) return rc;
   }
   return EW_OK;
 }

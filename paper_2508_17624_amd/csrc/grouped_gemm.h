@@ -11,24 +11,43 @@ enum { kWF32 = 0, kWBf16 = 1, kW4 = 2 };  // how weights (kWgrad: rows) are held
 
 struct GemmArgs {
   GroupedRows g;
-  const void* x;      // token rows
+  const void* x;      // token rows, x_rows of them
   const void* w;      // weights of slot 0; kWgrad: dy
   void* out;
   size_t slot_bytes;  // of a slot's weights
+  const float* h;     // kEpBack: [rows, 2N] the first product's sums
+  void* dh;           // kEpBack: [rows, 2N], in the rows' type
   int K, N;           // kWgrad: K is x's width, N is dy's
+  int x_rows;
   int first_slot, num_slots, accumulate;  // kWgrad
 };
+
+// What becomes of a product's sums.
+enum { kEpBf16 = 0, kEpF32 = 1,
+       kEpSwiglu = 2,   // out[r][n] = silu(g) u (bf16), weights [2N, K]: gate rows, then up rows
+       kEpBack = 3 };   // sums are da: out[r][n] = a, dh[r] = [dg, du], from g and u in h (grouped_backward.hip)
 
 // Bytes of an expert's [N, K] weights in 4 bits: codes [N, K/2], then scales [N, K/32].
 inline size_t w4_bytes(long long N, long long K) { return (size_t)(N * (K / 2) + N * (K / 32)); }
 __host__ __device__ __forceinline__ size_t w4_scales_at(int N, int K) { return (size_t)N * (K / 2); }
 
-// grouped_gemm.hip: any sizes and alignments.
-int launch_gemm_any(int way, int weights, bool bf16_rows, bool out_f32, const GemmArgs& a, hipStream_t st);
-// grouped_gemm.hip: the kernel for these arguments.
-int launch_gemm(int way, int weights, bool bf16_rows, bool out_f32, const GemmArgs& a, hipStream_t st);
+// grouped_gemm.hip: any sizes and alignments.  bf16: rows and results (but for kEpF32's).
+int launch_gemm_any(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st);
+// grouped_tile.hip: bf16 matrix cores; whether it takes these arguments.
+bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a);
+int launch_tile(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st);
+// grouped_gemm.hip: by the kernel for these arguments.
+int launch_gemm(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st);
+
+// a = silu(g) u, and from da the gradients of g and u (kEpBack).
+struct SwigluBack { float a, dg, du; };
+__device__ __forceinline__ SwigluBack swiglu_back(float g, float u, float da) {
+  const float s = 1.f / (1.f + __expf(-g)), gs = g * s;
+  return {gs * u, da * u * (s + gs * (1.f - s)), da * gs};
+}
+__device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
 // Checks what every call over sorted rows needs; 0 or an error.
-int check_rows(const char* who, int num_rows, int k, int P, const void* counts, const void* offsets);
+int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets);
 
 }  // namespace ew

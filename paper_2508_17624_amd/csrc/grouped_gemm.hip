@@ -30,8 +30,9 @@ constexpr int kTile = 64, kStep = 16, kPitch = kTile + 4;
 
 // Four elements of an operand, fp32: element (o + i, kk) for i < 4 where ALONG_O, otherwise (o, kk + i).
 // TW: type of the elements; float, uint16_t (bf16), or uint8_t for a 4-bit expert's bytes.
-template <int WAY, typename TX, typename TW>
-__global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n, int out_f32) {
+template <int WAY, typename TX, typename TW, int EP>
+__global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n) {
+  constexpr bool GATED = EP == kEpSwiglu;  // 32 features: tile index 16 q + 8 s + r is feature 8 q + r of the gate (s = 0) or up rows
   __shared__ float s_a[kStep][kPitch], s_b[kStep][kPitch];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tile = blockIdx.x % tiles_n, unit = blockIdx.x / tiles_n;
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n, int o
   } else {
     ch = find_chunk<kTile, 1>(a.g, unit);
     if (ch.slot < 0) return;
-    a0 = tile * kTile; b0 = 0;
+    a0 = tile * (GATED ? kTile / 2 : kTile); b0 = 0;
     na = N; nb = ch.rows; len = K;
   }
   const TX* x = (const TX*)a.x;
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n, int o
     if constexpr (WAY == kWgrad) return as_f32(x[(size_t)source_row(a.g, ch.first + kk) * K + o]);
     else if constexpr (sizeof(TW) == 1) {
       const uint32_t two = ws[(size_t)o * (K / 2) + kk / 2];
-      return w4_value(kk & 1 ? two >> 4 : two & 15, ws[w4_scales_at(N, K) + (size_t)o * (K / 32) + kk / 32]);
+      return w4_value(kk & 1 ? two >> 4 : two & 15, ws[w4_scales_at(GATED ? 2 * N : N, K) + (size_t)o * (K / 32) + kk / 32]);
     } else return as_f32(((const TW*)ws)[WAY == kFwd ? (size_t)o * K + kk : (size_t)kk * N + o]);
   };
   const int row_k = tid >> 2, k_k = (tid & 3) * 4;   // a thread's four elements along the contraction
@@ -72,8 +73,8 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n, int o
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (WAY == kFwd) {
-        const int o = a0 + row_k, kk = k0 + k_k + i;
-        va[i] = o < na && kk < len ? at_a(o, kk) : 0.f;
+        const int o = a0 + (GATED ? 8 * (row_k >> 4) + (row_k & 7) : row_k), kk = k0 + k_k + i;
+        va[i] = o < na && kk < len ? at_a(GATED && (row_k & 8) ? o + N : o, kk) : 0.f;
       } else {
         const int o = a0 + row_o + i, kk = k0 + k_o;
         va[i] = o < na && kk < len ? at_a(o, kk) : 0.f;
@@ -101,64 +102,87 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n, int o
   // lane l: B element l % 32, A elements 8 (i / 4) + 4 (l / 32) + i % 4
   const int b = b0 + (wave >> 1) * 32 + (lane & 31);
   if (b >= nb) return;
-  const size_t at = WAY == kWgrad ? ((size_t)unit * N + b) * K : (size_t)(ch.first + b) * N;
+  const size_t row = WAY == kWgrad ? (size_t)unit * N + b : (size_t)(ch.first + b);
+  if constexpr (GATED) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int o = a0 + (wave & 1) * 16 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+      if (o < na) put((TX*)a.out + row * N + o, swiglu(acc[8 * (i >> 2) + (i & 3)], acc[8 * (i >> 2) + 4 + (i & 3)]));
+    }
+    return;
+  }
+  const size_t at = row * (WAY == kWgrad ? K : N);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int o = a0 + (wave & 1) * 32 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
     if (o >= na) continue;
-    if (out_f32) {
+    if constexpr (EP == kEpBack) {
+      const SwigluBack v = swiglu_back(a.h[row * 2 * N + o], a.h[row * 2 * N + N + o], acc[i]);
+      put((TX*)a.out + at + o, v.a);
+      put((TX*)a.dh + row * 2 * N + o, v.dg);
+      put((TX*)a.dh + row * 2 * N + N + o, v.du);
+    } else if constexpr (EP == kEpF32) {
       float* p = (float*)a.out + at + o;
-      put(p, WAY == kWgrad && a.accumulate ? *p + acc[i] : acc[i]);
+      *p = WAY == kWgrad && a.accumulate ? *p + acc[i] : acc[i];
     } else {
       put((uint16_t*)a.out + at + o, acc[i]);
     }
   }
 }
 
-template <int WAY, typename TX, typename TW>
-int launch_any(const GemmArgs& a, bool out_f32, hipStream_t st) {
+template <int WAY, typename TX, typename TW, int EP>
+int launch_any(const GemmArgs& a, hipStream_t st) {
   long long units, tiles;
   if (WAY == kWgrad) {
     units = a.num_slots;
     tiles = (long long)ceil_div(a.K, kTile) * ceil_div(a.N, kTile);
   } else {
     units = max_chunks(a.g.rows, a.g.P, kTile);
-    tiles = ceil_div(a.N, kTile);
+    tiles = ceil_div(a.N, EP == kEpSwiglu ? kTile / 2 : kTile);
   }
   if (units * tiles >= (1ll << 31)) return fail(EW_ERR_UNSUPPORTED, "grouped product: too many output tiles for one launch");
   if (units * tiles == 0) return EW_OK;
-  hipLaunchKernelGGL((k_gemm_any<WAY, TX, TW>), dim3((unsigned)(units * tiles)), dim3(256), 0, st, a, (int)tiles, (int)out_f32);
+  hipLaunchKernelGGL((k_gemm_any<WAY, TX, TW, EP>), dim3((unsigned)(units * tiles)), dim3(256), 0, st, a, (int)tiles);
   EW_LAUNCH_CHECK("k_gemm_any");
   return EW_OK;
 }
 
+// In the rows' type, or fp32.
+template <int WAY, typename TW>
+int launch_any_bf16(int epilogue, const GemmArgs& a, hipStream_t st) {
+  return epilogue == kEpF32 ? launch_any<WAY, uint16_t, TW, kEpF32>(a, st) : launch_any<WAY, uint16_t, TW, kEpBf16>(a, st);
+}
+
 }  // namespace
 
-int launch_gemm_any(int way, int weights, bool bf16_rows, bool out_f32, const GemmArgs& a, hipStream_t st) {
-  if (weights == kW4) return launch_any<kFwd, uint16_t, uint8_t>(a, out_f32, st);
-  if (bf16_rows) {
-    if (way == kFwd) return launch_any<kFwd, uint16_t, uint16_t>(a, out_f32, st);
-    if (way == kDgrad) return launch_any<kDgrad, uint16_t, uint16_t>(a, out_f32, st);
-    return launch_any<kWgrad, uint16_t, uint16_t>(a, out_f32, st);
+int launch_gemm_any(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st) {
+  if (weights == kW4) return epilogue == kEpSwiglu ? launch_any<kFwd, uint16_t, uint8_t, kEpSwiglu>(a, st) : launch_any<kFwd, uint16_t, uint8_t, kEpBf16>(a, st);
+  if (epilogue == kEpBack) return bf16 ? launch_any<kDgrad, uint16_t, uint16_t, kEpBack>(a, st) : launch_any<kDgrad, float, float, kEpBack>(a, st);
+  if (bf16) {
+    if (way == kFwd) return launch_any_bf16<kFwd, uint16_t>(epilogue, a, st);
+    if (way == kDgrad) return launch_any<kDgrad, uint16_t, uint16_t, kEpBf16>(a, st);
+    return launch_any_bf16<kWgrad, uint16_t>(epilogue, a, st);
   }
-  if (way == kFwd) return launch_any<kFwd, float, float>(a, out_f32, st);
-  if (way == kDgrad) return launch_any<kDgrad, float, float>(a, out_f32, st);
-  return launch_any<kWgrad, float, float>(a, out_f32, st);
+  if (way == kFwd) return launch_any<kFwd, float, float, kEpF32>(a, st);
+  if (way == kDgrad) return launch_any<kDgrad, float, float, kEpF32>(a, st);
+  return launch_any<kWgrad, float, float, kEpF32>(a, st);
 }
 
-int launch_gemm(int way, int weights, bool bf16_rows, bool out_f32, const GemmArgs& a, hipStream_t st) {
-  return launch_gemm_any(way, weights, bf16_rows, out_f32, a, st);
+int launch_gemm(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st) {
+  if (tile_takes(way, weights, epilogue, a)) return launch_tile(way, weights, epilogue, a, st);
+  return launch_gemm_any(way, weights, epilogue, bf16, a, st);
 }
 
-int check_rows(const char* who, int num_rows, int k, int P, const void* counts, const void* offsets) {
-  if (num_rows < 0 || k < 1 || P < 1) return fail(EW_ERR_INVALID_ARG, "%s: need num_rows>=0, k>=1, P>=1 (got %d, %d, %d)", who, num_rows, k, P);
+int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets) {
+  if (num_tokens < 0 || num_rows < 0 || k < 1 || P < 1)
+    return fail(EW_ERR_INVALID_ARG, "%s: need num_tokens>=0, num_rows>=0, k>=1, P>=1 (got %d, %d, %d, %d)", who, num_tokens, num_rows, k, P);
   if (!counts || !offsets) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
   return EW_OK;
 }
 
 }  // namespace ew
 
-extern "C" int moe_grouped_gemm(const void* x, int dtype, int num_rows, int k, int K, int N, int P, int transposed,
+extern "C" int moe_grouped_gemm(const void* x, int dtype, int num_tokens, int num_rows, int k, int K, int N, int P, int transposed,
                                 const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row, const void* w_base, void* y,
                                 void* stream) {
   using ew::fail;
@@ -166,17 +190,17 @@ extern "C" int moe_grouped_gemm(const void* x, int dtype, int num_rows, int k, i
   if (K < 1 || N < 1) return fail(EW_ERR_INVALID_ARG, "%s: need K>=1, N>=1 (got %d, %d)", who, K, N);
   if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
-  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
   if (!x || !w_base || !y) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
   ew::GemmArgs a{};
   a.g = {counts, offsets, pair_of_row, P, num_rows, k};
-  a.x = x; a.w = w_base; a.out = y; a.K = K; a.N = N;
+  a.x = x; a.w = w_base; a.out = y; a.K = K; a.N = N; a.x_rows = num_tokens;
   a.slot_bytes = (size_t)N * K * (dtype == EW_BF16 ? 2 : 4);
-  return ew::launch_gemm(transposed ? ew::kDgrad : ew::kFwd, dtype == EW_BF16 ? ew::kWBf16 : ew::kWF32, dtype == EW_BF16, dtype == EW_F32, a,
-                         (hipStream_t)stream);
+  return ew::launch_gemm(transposed ? ew::kDgrad : ew::kFwd, dtype == EW_BF16 ? ew::kWBf16 : ew::kWF32,
+                         dtype == EW_BF16 ? ew::kEpBf16 : ew::kEpF32, dtype == EW_BF16, a, (hipStream_t)stream);
 }
 
-extern "C" int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_rows, int k, int K, int N, int P,
+extern "C" int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_tokens, int num_rows, int k, int K, int N, int P,
                                       const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row, int first_slot,
                                       int num_slots, int dw_dtype, int accumulate, void* dw, void* stream) {
   using ew::fail;
@@ -186,14 +210,15 @@ extern "C" int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, 
   if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
     return fail(EW_ERR_INVALID_ARG, "%s: dw is float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);
   if (accumulate && dw_dtype != EW_F32) return fail(EW_ERR_UNSUPPORTED, "%s: only float32 gradients accumulate", who);
-  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
   if (first_slot < 0 || num_slots < 0 || first_slot > P - num_slots)
     return fail(EW_ERR_INVALID_ARG, "%s: slots [%d, %d + %d) outside 0..P=%d", who, first_slot, first_slot, num_slots, P);
   if (num_slots == 0) return EW_OK;
   if (!dw || (num_rows > 0 && (!dy || !x))) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
   ew::GemmArgs a{};
   a.g = {counts, offsets, pair_of_row, P, num_rows, k};
-  a.x = x; a.w = dy; a.out = dw; a.K = K; a.N = N;
+  a.x = x; a.w = dy; a.out = dw; a.K = K; a.N = N; a.x_rows = num_tokens;
   a.first_slot = first_slot; a.num_slots = num_slots; a.accumulate = accumulate != 0;
-  return ew::launch_gemm(ew::kWgrad, dtype == EW_BF16 ? ew::kWBf16 : ew::kWF32, dtype == EW_BF16, dw_dtype == EW_F32, a, (hipStream_t)stream);
+  return ew::launch_gemm(ew::kWgrad, dtype == EW_BF16 ? ew::kWBf16 : ew::kWF32, dw_dtype == EW_F32 ? ew::kEpF32 : ew::kEpBf16, dtype == EW_BF16, a,
+                         (hipStream_t)stream);
 }

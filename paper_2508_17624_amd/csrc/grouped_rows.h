@@ -31,6 +31,23 @@ __device__ __forceinline__ int chunk_rows(int c) {
   return n <= 1 ? B : ((c + n - 1) / n + A - 1) / A * A;
 }
 
+// Chunks of all slots.  Every lane gets the answer.
+template <int B>
+__device__ __forceinline__ int count_chunks(const GroupedRows& g) {
+  int sum = 0;
+  for (int s = threadIdx.x & 63; s < g.P; s += 64) sum += (g.counts[s] + B - 1) / B;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  return __builtin_amdgcn_readfirstlane(sum);
+}
+
+// Workgroups go round the eight XCDs, each with an L2 of its own: unit `i` of `n` for this one so that an XCD works on one run of
+// neighbouring units (which share weights and rows).  Returns n where there is none left.
+__device__ __forceinline__ int unit_of_block(int n) {
+  const int per = (n + 7) / 8, i = (int)blockIdx.x >> 3, x = (int)blockIdx.x & 7;
+  return i < per ? min(n, x * per + i) : n;
+}
+
 // The chunk number `want` of all slots' chunks in slot order.  Every lane of the wave gets the same answer.  A lane looks at 8 slots,
 // the lanes' sums meet in one scan: two dependent round trips to L2 for up to 512 slots (about 1.5 us), the same for every chunk.
 template <int B, int A>

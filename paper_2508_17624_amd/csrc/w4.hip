@@ -81,17 +81,6 @@ __global__ __launch_bounds__(256) void k_dequantize_w4(const unsigned char* __re
   }
 }
 
-// act = silu(g) u of a row h = [g, u].
-__global__ __launch_bounds__(256) void k_swiglu(const int32_t* __restrict__ offsets, int P, int rows, int I, const float* __restrict__ h,
-                                                uint16_t* __restrict__ act) {
-  const long long n = (long long)min(rows, offsets[P]) * I;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
-    const long long r = i / I;
-    const float g = h[i + r * I], u = h[i + (r + 1) * I];
-    act[i] = __builtin_bit_cast(uint16_t, (__bf16)(g / (1.f + expf(-g)) * u));
-  }
-}
-
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // Common checks of packing and reading back; what both kernels step through, or 0 where there is nothing to do.
@@ -146,35 +135,36 @@ extern "C" int moe_dequantize_w4(const void* w4, int dtype, int num_experts, int
 
 namespace {
 
-ew::GemmArgs w4_args(const int32_t* counts, const int32_t* offsets, const int32_t* por, int P, int num_rows, int k, const void* x, const void* w, void* out,
-                     int K, int N) {
+ew::GemmArgs w4_args(const int32_t* counts, const int32_t* offsets, const int32_t* por, int P, int num_rows, int k, const void* x, int x_rows, const void* w,
+                     void* out, int K, int N, size_t slot_bytes) {
   ew::GemmArgs a{};
   a.g = {counts, offsets, por, P, num_rows, k};
-  a.x = x; a.w = w; a.out = out; a.K = K; a.N = N;
-  a.slot_bytes = moe_w4_expert_bytes(N, K);
+  a.x = x; a.x_rows = x_rows; a.w = w; a.out = out; a.K = K; a.N = N;
+  a.slot_bytes = slot_bytes;
   return a;
 }
 
 }  // namespace
 
-extern "C" int moe_grouped_gemm_w4(const void* x, int num_rows, int k, int K, int N, int P, const int32_t* counts, const int32_t* offsets,
+extern "C" int moe_grouped_gemm_w4(const void* x, int num_tokens, int num_rows, int k, int K, int N, int P, const int32_t* counts, const int32_t* offsets,
                                    const int32_t* pair_of_row, const void* w4_base, void* y, void* stream) {
   using ew::fail;
   const char* who = "moe_grouped_gemm_w4";
   if (K < 1 || N < 1) return fail(EW_ERR_INVALID_ARG, "%s: need K>=1, N>=1 (got %d, %d)", who, K, N);
   if (!moe_w4_expert_bytes(N, K)) return fail(EW_ERR_UNSUPPORTED, "%s: K must be a multiple of 32 and N*K of 512 (N=%d K=%d)", who, N, K);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
-  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
   if (!x || !w4_base || !y) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
-  return ew::launch_gemm(ew::kFwd, ew::kW4, true, false, w4_args(counts, offsets, pair_of_row, P, num_rows, k, x, w4_base, y, K, N), (hipStream_t)stream);
+  return ew::launch_gemm(ew::kFwd, ew::kW4, ew::kEpBf16, true,
+                         w4_args(counts, offsets, pair_of_row, P, num_rows, k, x, num_tokens, w4_base, y, K, N, moe_w4_expert_bytes(N, K)), (hipStream_t)stream);
 }
 
 extern "C" size_t moe_grouped_ffn_w4_workspace_bytes(int num_rows, int I) {
   if (num_rows < 1 || I < 1) return 0;
-  return ew::align_up((size_t)num_rows * I * 2, 256) + ew::align_up((size_t)num_rows * I * 8, 256);
+  return ew::align_up((size_t)num_rows * I * 2, 256);
 }
 
-extern "C" int moe_grouped_ffn_w4(const void* x, int num_rows, int k, int H, int I, int P, const int32_t* counts, const int32_t* offsets,
+extern "C" int moe_grouped_ffn_w4(const void* x, int num_tokens, int num_rows, int k, int H, int I, int P, const int32_t* counts, const int32_t* offsets,
                                   const int32_t* pair_of_row, const void* w13_base, const void* w2_base, void* y_sorted, void* ws,
                                   size_t ws_bytes, void* stream) {
   using ew::fail;
@@ -183,17 +173,15 @@ extern "C" int moe_grouped_ffn_w4(const void* x, int num_rows, int k, int H, int
   if (!moe_w4_expert_bytes(2 * I, H) || !moe_w4_expert_bytes(H, I))
     return fail(EW_ERR_UNSUPPORTED, "%s: H and I must be multiples of 32 and H*I of 512 (H=%d I=%d)", who, H, I);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
-  if (const int rc = ew::check_rows(who, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
   if (!x || !w13_base || !w2_base || !y_sorted) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
   const size_t need = moe_grouped_ffn_w4_workspace_bytes(num_rows, I);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
     return fail(EW_ERR_WORKSPACE, "%s: workspace needs %zu bytes aligned to 256 (got %zu at %p)", who, need, ws_bytes, ws);
   const hipStream_t st = (hipStream_t)stream;
-  uint16_t* act = (uint16_t*)ws;
-  float* h = (float*)((char*)ws + ew::align_up((size_t)num_rows * I * 2, 256));
-  int rc = ew::launch_gemm(ew::kFwd, ew::kW4, true, true, w4_args(counts, offsets, pair_of_row, P, num_rows, k, x, w13_base, h, H, 2 * I), st);
+  const int rc = ew::launch_gemm(ew::kFwd, ew::kW4, ew::kEpSwiglu, true,
+                                 w4_args(counts, offsets, pair_of_row, P, num_rows, k, x, num_tokens, w13_base, ws, H, I, moe_w4_expert_bytes(2 * I, H)), st);
   if (rc) return rc;
-  hipLaunchKernelGGL(ew::k_swiglu, dim3((unsigned)ew::pack_grid((long long)num_rows * I)), dim3(256), 0, st, offsets, P, num_rows, I, h, act);
-  EW_LAUNCH_CHECK("k_swiglu");
-  return ew::launch_gemm(ew::kFwd, ew::kW4, true, false, w4_args(counts, offsets, nullptr, P, num_rows, 1, act, w2_base, y_sorted, I, H), st);
+  return ew::launch_gemm(ew::kFwd, ew::kW4, ew::kEpBf16, true,
+                         w4_args(counts, offsets, nullptr, P, num_rows, 1, ws, num_rows, w2_base, y_sorted, I, H, moe_w4_expert_bytes(H, I)), st);
 }

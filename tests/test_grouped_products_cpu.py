@@ -13,22 +13,22 @@ ONE = C.c_void_p(256)   # never dereferenced
 INVALID, WORKSPACE, UNSUPPORTED = -1, -5, -6
 
 
-def gemm(x=ONE, dtype=ew.EW_BF16, rows=4, k=2, K=8, N=8, P=3, counts=ONE, offsets=ONE, w=ONE, y=ONE):
-    return ew.lib().moe_grouped_gemm(x, dtype, rows, k, K, N, P, 0, counts, offsets, None, w, y, None)
+def gemm(x=ONE, dtype=ew.EW_BF16, tokens=4, rows=4, k=2, K=8, N=8, P=3, counts=ONE, offsets=ONE, w=ONE, y=ONE):
+    return ew.lib().moe_grouped_gemm(x, dtype, tokens, rows, k, K, N, P, 0, counts, offsets, None, w, y, None)
 
 
 def wgrad(dy=ONE, x=ONE, dtype=ew.EW_BF16, rows=4, k=2, K=8, N=8, P=3, counts=ONE, first=0, n=3, dw_dtype=ew.EW_F32, accumulate=0, dw=ONE):
-    return ew.lib().moe_grouped_gemm_wgrad(dy, x, dtype, rows, k, K, N, P, counts, ONE, None, first, n, dw_dtype, accumulate, dw, None)
+    return ew.lib().moe_grouped_gemm_wgrad(dy, x, dtype, 4, rows, k, K, N, P, counts, ONE, None, first, n, dw_dtype, accumulate, dw, None)
 
 
 def backward(dtype=ew.EW_BF16, rows=4, H=8, I=8, P=3, dx=ONE, first=0, n=3, dw_dtype=ew.EW_F32, accumulate=0, d13=ONE, ws=ONE, ws_bytes=1 << 30, x=ONE):
-    return ew.lib().moe_grouped_ffn_backward(x, ONE, dtype, rows, 2, H, I, P, ONE, ONE, None, ONE, ONE, dx, first, n, dw_dtype, accumulate, d13, ONE, ws,
+    return ew.lib().moe_grouped_ffn_backward(x, ONE, dtype, 4, rows, 2, H, I, P, ONE, ONE, None, ONE, ONE, dx, first, n, dw_dtype, accumulate, d13, ONE, ws,
                                              ws_bytes, None)
 
 
 def test_grouped_products_refuse_on_the_host():
     for bad in (dict(x=None), dict(w=None), dict(y=None), dict(counts=None), dict(offsets=None), dict(dtype=2), dict(K=0), dict(N=0), dict(P=0), dict(k=0),
-                dict(rows=-1)):
+                dict(rows=-1), dict(tokens=-1)):
         assert gemm(**bad) == INVALID and b"moe_grouped_gemm" in ew.lib().ew_last_error(), bad
     assert gemm(rows=0) == 0 and gemm(rows=0, x=None, y=None, w=None) == 0     # no rows: nothing to do
     for bad in (dict(dy=None), dict(dw=None), dict(counts=None), dict(dtype=9), dict(dw_dtype=5), dict(dtype=ew.EW_F32, dw_dtype=ew.EW_BF16), dict(first=-1),
@@ -65,16 +65,16 @@ def test_four_bit_calls_refuse_on_the_host():
         assert call(ONE, 4, 2, 16, 64, ONE, None) == INVALID and call(ONE, 1, -1, 16, 64, ONE, None) == INVALID
         assert call(C.c_void_p(264), 1, 2, 16, 64, ONE, None) == INVALID        # not aligned to 16 bytes
         assert call(None, 1, 0, 16, 64, None, None) == 0
-    assert lib.moe_grouped_gemm_w4(ONE, 4, 2, 40, 16, 3, ONE, ONE, None, ONE, ONE, None) == UNSUPPORTED
-    assert lib.moe_grouped_gemm_w4(ONE, 4, 2, 64, 16, 3, ONE, ONE, None, None, ONE, None) == INVALID
-    assert lib.moe_grouped_gemm_w4(ONE, 0, 2, 64, 16, 3, None, None, None, None, None, None) == 0
+    assert lib.moe_grouped_gemm_w4(ONE, 4, 4, 2, 40, 16, 3, ONE, ONE, None, ONE, ONE, None) == UNSUPPORTED
+    assert lib.moe_grouped_gemm_w4(ONE, 4, 4, 2, 64, 16, 3, ONE, ONE, None, None, ONE, None) == INVALID
+    assert lib.moe_grouped_gemm_w4(ONE, 0, 0, 2, 64, 16, 3, None, None, None, None, None, None) == 0
     ffn = lib.moe_grouped_ffn_w4
     need = lib.moe_grouped_ffn_w4_workspace_bytes(4, 128)
     assert need >= 4 * 128 * 2 and lib.moe_grouped_ffn_w4_workspace_bytes(0, 128) == 0
-    assert ffn(ONE, 4, 2, 128, 40, 3, ONE, ONE, None, ONE, ONE, ONE, ONE, need, None) == UNSUPPORTED
-    assert ffn(ONE, 4, 2, 128, 128, 3, ONE, ONE, None, ONE, ONE, ONE, ONE, need - 1, None) == WORKSPACE
-    assert ffn(ONE, 4, 2, 128, 128, 3, ONE, ONE, None, ONE, ONE, ONE, None, need, None) == WORKSPACE
-    assert ffn(ONE, 4, 2, 128, 128, 3, ONE, ONE, None, None, ONE, ONE, ONE, need, None) == INVALID
+    assert ffn(ONE, 4, 4, 2, 128, 40, 3, ONE, ONE, None, ONE, ONE, ONE, ONE, need, None) == UNSUPPORTED
+    assert ffn(ONE, 4, 4, 2, 128, 128, 3, ONE, ONE, None, ONE, ONE, ONE, ONE, need - 1, None) == WORKSPACE
+    assert ffn(ONE, 4, 4, 2, 128, 128, 3, ONE, ONE, None, ONE, ONE, ONE, None, need, None) == WORKSPACE
+    assert ffn(ONE, 4, 4, 2, 128, 128, 3, ONE, ONE, None, None, ONE, ONE, ONE, need, None) == INVALID
 
 
 def test_bindings_refuse_what_does_not_fit():
