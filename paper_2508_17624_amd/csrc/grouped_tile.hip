@@ -1,7 +1,8 @@
 // Matrix products grouped by expert on the bf16 matrix cores, many rows per slot: forward, input gradient, weight gradient.
 //
 // A workgroup makes one tile of TA outputs along the contiguous axis of the result ("features", operand A) times up to TB along the
-// other ("rows", operand B) with v_mfma_f32_32x32x16_bf16: waves of 64 features x half of the rows, two per SIMD.
+// other ("rows", operand B) with v_mfma_f32_32x32x16_bf16, four waves of half of the features x half of the rows: at 256 x 256 a wave's 128 x 128
+// sums fill half of its registers and 8 operand reads feed 16 MFMAs (eight waves of 64 x 128: 6 for 8, 2 to 5 % slower).
 // The contraction comes in slabs of 64 through an LDS ring, filled by LDS-direct loads while earlier slabs are multiplied.
 //
 // An operand lies in memory along the contraction (x, and w of the forward product) or across it (w of the input gradient, both
@@ -68,13 +69,14 @@ struct Cfg {
   static constexpr bool MAPPED = MAPPED_;                            // rows of x are looked up
   static constexpr bool A_ACROSS = WAY != kFwd, B_ACROSS = WAY == kWgrad;
   static constexpr bool GATED = EP == kEpSwiglu;
-  static constexpr int WAVES = TA / 32, THREADS = 64 * WAVES;        // TA / 64 parts of the features x two halves of the rows
-  static constexpr int MA = 2, MB = TB / 64;                         // a wave's fragments; row fragment f of half b is rows 32 (b + 2 f) ..
+  static constexpr int WAVES = 4, THREADS = 64 * WAVES;        // two halves of the features x two halves of the rows
+  static constexpr int MA = TA / 64, MB = TB / 64;                         // a wave's fragments; row fragment f of half b is rows 32 (b + 2 f) ..
   static constexpr int UNIT = TA * kSlab * 2, RING = 5, LDS = RING * UNIT;
   static constexpr int NL = UNIT / 1024 / WAVES;                     // load instructions of a wave for one operand's slab
   static constexpr int ROW = TA * 2;                                 // bytes of an LDS row across the contraction
   static constexpr int PPR = TA / 8, RPI = 64 / PPR;                 // its pieces of 16 bytes; rows of a load instruction
-  static_assert(TA == TB && LDS * 8 <= 160 * 1024 * WAVES, "LDS budget of a CU: room for eight waves, two per SIMD");
+  static constexpr int WPE = TA == 256 ? 1 : 2;                      // waves per SIMD: what LDS has room for
+  static_assert(TA == TB && LDS * WPE <= 160 * 1024, "LDS budget of a CU");
   // first LDS row, along the contraction, of feature fragment i of half a
   static constexpr int feature_row(int a, int i) { return GATED ? (i < MA / 2 ? 0 : TA / 2) + a * (MA / 2) * 32 + i % (MA / 2) * 32 : (a * MA + i) * 32; }
 };
@@ -122,7 +124,8 @@ __device__ __forceinline__ void multiply(int nk, const uint32_t (&fa)[C::MA], co
     };
     read_a(std::integral_constant<int, 0>{}); read_b(std::integral_constant<int, 0>{});
     read_a(std::integral_constant<int, 1>{}); read_b(std::integral_constant<int, 1>{});
-    read_b(std::integral_constant<int, 2>{}); read_b(std::integral_constant<int, 3>{});
+    read_a(std::integral_constant<int, 2>{}); read_b(std::integral_constant<int, 2>{});
+    read_a(std::integral_constant<int, 3>{}); read_b(std::integral_constant<int, 3>{});
   };
   auto landed = [&](auto c_tag) {
     constexpr int c = decltype(c_tag)::value;
@@ -176,7 +179,7 @@ __device__ __forceinline__ void idle(int nk, Step step, Load load) {  // a wave 
 }
 
 template <typename C>
-__global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_tile(GemmArgs a, int tiles_a, int units, uint32_t by_k) {
+__global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::WPE, C::WPE))) void k_tile(GemmArgs a, int tiles_a, int units, uint32_t by_k) {
   __shared__ __attribute__((aligned(1024))) unsigned char s_lds[C::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int K = a.K, N = a.N;
