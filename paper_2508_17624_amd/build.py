@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libexpertweave.so")
 SOURCES = ["errors.cpp", "pool.cpp", "route_permute.hip", "unpermute_gate.hip", "ffn.hip", "ffn_gemm.hip", "ffn_f32.hip", "ffn_plan.hip", "ffn_dec.hip", "ffn_big.hip", "layer.cpp", "probe.hip",
-           "grouped_gemm.hip", "grouped_tile.hip", "grouped_backward.hip", "w4.hip"]
+           "grouped_gemm.hip", "grouped_tile.hip", "grouped_stream.hip", "grouped_backward.hip", "w4.hip"]
 
 
 def hipcc() -> str:

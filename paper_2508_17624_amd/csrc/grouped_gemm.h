@@ -33,6 +33,9 @@ __host__ __device__ __forceinline__ size_t w4_scales_at(int N, int K) { return (
 
 // grouped_gemm.hip: any sizes and alignments.  bf16: rows and results (but for kEpF32's).
 int launch_gemm_any(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st);
+// grouped_stream.hip: few rows per slot, bf16 or 4-bit weights; whether it takes these arguments.
+bool stream_takes(int way, int weights, int epilogue, const GemmArgs& a);
+int launch_stream(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st);
 // grouped_tile.hip: bf16 matrix cores; whether it takes these arguments.
 bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a);
 int launch_tile(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st);

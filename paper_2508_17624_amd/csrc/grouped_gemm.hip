@@ -169,6 +169,7 @@ int launch_gemm_any(int way, int weights, int epilogue, bool bf16, const GemmArg
 }
 
 int launch_gemm(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st) {
+  if (stream_takes(way, weights, epilogue, a)) return launch_stream(way, weights, epilogue, a, st);
   if (tile_takes(way, weights, epilogue, a)) return launch_tile(way, weights, epilogue, a, st);
   return launch_gemm_any(way, weights, epilogue, bf16, a, st);
 }

@@ -63,10 +63,11 @@ struct Frag<true> {
   __device__ __forceinline__ bf16x8 get() const { return __builtin_bit_cast(bf16x8, (u32x4){lo[0], lo[1], hi[0], hi[1]}); }
 };
 
-template <int WAY_, int TA_, int TB_, int EP_, bool MAPPED_>
+template <int WAY_, int TA_, int TB_, int EP_, bool MAPPED_, bool W4_>
 struct Cfg {
   static constexpr int WAY = WAY_, TA = TA_, TB = TB_, EP = EP_;
   static constexpr bool MAPPED = MAPPED_;                            // rows of x are looked up
+  static constexpr bool W4 = W4_;                                    // weights in 4 bits
   static constexpr bool A_ACROSS = WAY != kFwd, B_ACROSS = WAY == kWgrad;
   static constexpr bool GATED = EP == kEpSwiglu;
   static constexpr int WAVES = 4, THREADS = 64 * WAVES;        // two halves of the features x two halves of the rows
@@ -77,6 +78,7 @@ struct Cfg {
   static constexpr int PPR = TA / 8, RPI = 64 / PPR;                 // its pieces of 16 bytes; rows of a load instruction
   static constexpr int WPE = TA == 256 ? 1 : 2;                      // waves per SIMD: what LDS has room for
   static_assert(TA == TB && LDS * WPE <= 160 * 1024, "LDS budget of a CU");
+  static constexpr int PARTS = TA / 128;                             // W4: 16-byte pieces of codes of a thread and slab
   // first LDS row, along the contraction, of feature fragment i of half a
   static constexpr int feature_row(int a, int i) { return GATED ? (i < MA / 2 ? 0 : TA / 2) + a * (MA / 2) * 32 + i % (MA / 2) * 32 : (a * MA + i) * 32; }
 };
@@ -136,7 +138,7 @@ __device__ __forceinline__ void multiply(int nk, const uint32_t (&fa)[C::MA], co
     for (int f = 0; f < NBF; ++f) b[c][f].landed();
   };
   constexpr int PER = 2 * C::NL / 4;  // loads of a k-step, behind groups of MFMAs
-  auto mul = [&](auto c_tag, auto part_tag) {
+  auto mul = [&](auto c_tag, auto part_tag, auto odd_tag) {
     constexpr int c = decltype(c_tag)::value, part = decltype(part_tag)::value;
 #pragma unroll
     for (int f = 0; f < NBF; ++f) {
@@ -146,7 +148,7 @@ __device__ __forceinline__ void multiply(int nk, const uint32_t (&fa)[C::MA], co
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int q = 0; q < PER; ++q)
-          if (q * NBF / PER == f) load(part * PER + q);
+          if (q * NBF / PER == f) load(part * PER + q, odd_tag);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -160,21 +162,34 @@ __device__ __forceinline__ void multiply(int nk, const uint32_t (&fa)[C::MA], co
   for (int i = 0; i < C::MA; ++i) a[1][i] = {};
 #pragma unroll
   for (int f = 0; f < NBF; ++f) b[1][f] = {};
-  for (int kt = 0; kt < nk; ++kt) {
+  auto slab = [&](int kt, auto odd) {
     at = step(kt);
-    read(_0, _0); mul(_1, _0); landed(_0);
-    read(_1, _1); mul(_0, _1); landed(_1);
-    read(_0, _2); mul(_1, _2); landed(_0);
-    read(_1, _3); mul(_0, _3); landed(_1);
+    read(_0, _0); mul(_1, _0, odd); landed(_0);
+    read(_1, _1); mul(_0, _1, odd); landed(_1);
+    read(_0, _2); mul(_1, _2, odd); landed(_0);
+    read(_1, _3); mul(_0, _3, odd); landed(_1);
+  };
+  if constexpr (C::W4) {
+    for (int kt = 0; kt < nk; kt += 2) {  // (an even number: K % 128 == 0)
+      slab(kt, _0);
+      slab(kt + 1, _1);
+    }
+  } else {
+    for (int kt = 0; kt < nk; ++kt) slab(kt, _0);
   }
-  mul(_1, std::integral_constant<int, -1>{});
+  mul(_1, std::integral_constant<int, -1>{}, _0);
 }
 template <typename C, typename Step, typename Load>
 __device__ __forceinline__ void idle(int nk, Step step, Load load) {  // a wave without rows keeps loading
-  for (int kt = 0; kt < nk; ++kt) {
+  auto slab = [&](int kt, auto odd) {
     step(kt);
 #pragma unroll
-    for (int q = 0; q < 2 * C::NL; ++q) load(q);
+    for (int q = 0; q < 2 * C::NL; ++q) load(q, odd);
+    wait_lds();
+  };
+  for (int kt = 0; kt < nk; kt += C::W4 ? 2 : 1) {
+    slab(kt, std::integral_constant<int, 0>{});
+    if constexpr (C::W4) slab(kt + 1, std::integral_constant<int, 1>{});
   }
 }
 
@@ -283,6 +298,44 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     for (int n = 0; n < C::NL; ++n)
       if (kt * kSlab + ((lane & 7) ^ swz<decltype(features)::value>(along_row(n))) * 8 >= K) off[n] = kNowhere;
   };
+  // W4: a thread fetches 32 or 16 bytes of codes of one feature two slabs ahead, and turns them into bf16 in LDS a slab ahead of their use.
+  const int w4_row = C::PARTS == 2 ? (int)threadIdx.x : (int)threadIdx.x >> 1, w4_half = C::PARTS == 2 ? 0 : (int)threadIdx.x & 1;
+  uint32_t w4_codes = kNowhere, w4_scales = kNowhere;
+  u32x4 codes[2][C::PARTS];
+  uint32_t scales[2] = {};
+  if constexpr (C::W4) {
+    const int f = a0 + (C::GATED && w4_row >= C::TA / 2 ? w4_row - C::TA / 2 : w4_row);
+    const uint32_t row = (uint32_t)(C::GATED && w4_row >= C::TA / 2 ? f + N : f);
+    if (f < N) {
+      w4_codes = row * (uint32_t)(K / 2) + 16 * w4_half;
+      w4_scales = (uint32_t)w4_scales_at(C::GATED ? 2 * N : N, K) + row * (uint32_t)(K / 32) + w4_half;
+    }
+  }
+  auto fetch = [&](int kt, auto odd) {
+    if constexpr (C::W4) {
+      constexpr int o = decltype(odd)::value;
+      const Rsrc r = resource(pa, kt < nk ? na_bytes : 0u);
+#pragma unroll
+      for (int p = 0; p < C::PARTS; ++p)
+        codes[o][p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)w4_codes, kt * (kSlab / 2) + 16 * p, 0));
+      if constexpr (C::PARTS == 2) scales[o] = __builtin_amdgcn_raw_buffer_load_b16(r, (int)w4_scales, kt * (kSlab / 32), 0);
+      else scales[o] = __builtin_amdgcn_raw_buffer_load_b8(r, (int)w4_scales, kt * (kSlab / 32), 0);
+    }
+  };
+  auto stage = [&](int unit, int n, auto odd) {  // piece n (of 4 PARTS) of the thread's codes
+    if constexpr (C::W4) {
+      constexpr int o = decltype(odd)::value;
+      const float scale = __uint_as_float((scales[o] >> (8 * (n >> 2)) & 255u) << 23);
+      const uint32_t word = codes[o][C::PARTS == 2 ? n >> 2 : 0][n & 3];
+      u32x4 v;
+      v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
+      v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
+      v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
+      v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
+      const uint32_t at = (uint32_t)(uintptr_t)(lds_byte*)s_lds + unit * C::UNIT + w4_row * 128 + ((4 * w4_half + n) ^ swz<true>(w4_row)) * 16;
+      asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v));
+    }
+  };
   auto load_a = [&](int kt, int unit, int n) {
     load_lds(resource(pa, kt < nk ? na_bytes : 0u), lds_at(unit, n), C::WAY == kWgrad && C::MAPPED ? step_a[C::WAY == kWgrad ? n : 0] : oa[n], (uint32_t)kt * sa);
   };
@@ -315,24 +368,40 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   // are on their way (weights come from farther than rows).
   int slab = 0, now = 0;  // unit of slab `now`'s A
   auto unit_of = [&](int ahead) { return slab + ahead >= C::RING ? slab + ahead - C::RING : slab + ahead; };
+  if constexpr (C::W4) {
+    fetch(0, std::integral_constant<int, 0>{});
+    fetch(1, std::integral_constant<int, 1>{});
+    in_order();
+  }
   look_up(0);
   look_up(1);
   if constexpr (!C::A_ACROSS) cut_tail(oa, 0, std::true_type{});
   if constexpr (!C::B_ACROSS) cut_tail(ob, 0, std::false_type{});
   in_order();
+  if constexpr (!C::W4) {
 #pragma unroll
-  for (int n = 0; n < C::NL; ++n) load_a(0, 0, n);
+    for (int n = 0; n < C::NL; ++n) load_a(0, 0, n);
+  }
 #pragma unroll
   for (int n = 0; n < C::NL; ++n) load_b(0, 1, n);
   in_order();
   look_up(2);
   if constexpr (!C::A_ACROSS) cut_tail(oa, 1, std::true_type{});
   in_order();
+  if constexpr (C::W4) {
 #pragma unroll
-  for (int n = 0; n < C::NL; ++n) load_a(1, 2, n);
-  in_order();
+    for (int n = 0; n < 4 * C::PARTS; ++n) stage(0, n, std::integral_constant<int, 0>{});
+    in_order();
+    fetch(2, std::integral_constant<int, 0>{});
+    in_order();
+    wait_lds();
+  } else {
+#pragma unroll
+    for (int n = 0; n < C::NL; ++n) load_a(1, 2, n);
+    in_order();
+  }
   auto step = [&](int kt) -> Slab {
-    wait_mem<C::NL>();  // all but A of slab kt + 1
+    wait_mem<C::W4 ? C::PARTS + 1 : C::NL>();  // all but A of slab kt + 1 (W4: the codes of slab kt + 2)
     __builtin_amdgcn_s_barrier();
     if (kt) slab = unit_of(2);
     now = kt;
@@ -340,8 +409,21 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     if constexpr (!C::B_ACROSS) cut_tail(ob, kt + 1, std::false_type{});
     return {(uint32_t)(slab * C::UNIT), (uint32_t)(unit_of(1) * C::UNIT)};
   };
-  auto load = [&](int q) {  // B of the next slab, then A of the one behind it
-    if (q < C::NL) {
+  auto load = [&](int q, auto odd) {  // B of the next slab, then A of the one behind it (W4: A of the next slab into LDS, and the codes two behind it)
+    if constexpr (C::W4) {
+      using Next = std::integral_constant<int, 1 - decltype(odd)::value>;
+      if (q < C::NL) {
+        load_b(now + 1, unit_of(3), q);
+        if (q == C::NL - 1) in_order();
+      } else {
+        if (q - C::NL < 4 * C::PARTS) stage(unit_of(2), q - C::NL, Next{});
+        if (q == 2 * C::NL - 1) {
+          in_order();
+          fetch(now + 3, Next{});
+          in_order();
+        }
+      }
+    } else if (q < C::NL) {
       load_b(now + 1, unit_of(3), q);
     } else {
       if (q == C::NL) {
@@ -450,9 +532,9 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   }
 }
 
-template <int WAY, int TA, int TB, int EP, bool MAPPED>
+template <int WAY, int TA, int TB, int EP, bool MAPPED, bool W4 = false>
 int launch_cfg(const GemmArgs& a, hipStream_t st) {
-  using C = Cfg<WAY, TA, TB, EP, MAPPED>;
+  using C = Cfg<WAY, TA, TB, EP, MAPPED, W4>;
   long long units;
   int tiles_a;
   if (WAY == kWgrad) {
@@ -474,22 +556,24 @@ int launch_cfg(const GemmArgs& a, hipStream_t st) {
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // The larger tile where a slot has more than 128 rows on average (the weight gradient: wherever the outputs fill it).
-template <int WAY, int EP, bool MAPPED>
+template <int WAY, int EP, bool MAPPED, bool W4>
 int launch_sized(const GemmArgs& a, hipStream_t st) {
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;
   const bool large = WAY == kWgrad ? (long long)a.K * a.N > 512 * 512 : a.g.rows > 64 * used && a.N > 128;
-  return large ? launch_cfg<WAY, 256, 256, EP, MAPPED>(a, st) : launch_cfg<WAY, 128, 128, EP, MAPPED>(a, st);
+  return large ? launch_cfg<WAY, 256, 256, EP, MAPPED, W4>(a, st) : launch_cfg<WAY, 128, 128, EP, MAPPED, W4>(a, st);
 }
-template <int WAY, int EP>
+template <int WAY, int EP, bool W4 = false>
 int launch_mapped(const GemmArgs& a, hipStream_t st) {
-  return a.g.por || a.g.k > 1 ? launch_sized<WAY, EP, true>(a, st) : launch_sized<WAY, EP, false>(a, st);
+  return a.g.por || a.g.k > 1 ? launch_sized<WAY, EP, true, W4>(a, st) : launch_sized<WAY, EP, false, W4>(a, st);
 }
 
 }  // namespace
 
 bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   const unsigned long long lim = 1ull << 32;
-  if (weights != kWBf16 || a.K % 8 || a.N % 8 || !aligned16(a.x) || !aligned16(a.w) || !aligned16(a.out)) return false;
+  if (weights == kW4 ? way != kFwd || a.K % 128 || a.N % 16 : weights != kWBf16 || a.K % 8 || a.N % 8) return false;
+  if (epilogue == kEpSwiglu && weights != kW4) return false;
+  if (!aligned16(a.x) || !aligned16(a.w) || !aligned16(a.out)) return false;
   if (epilogue == kEpBack && (!aligned16(a.h) || !aligned16(a.dh))) return false;
   const bool mapped = a.g.por != nullptr || a.g.k > 1;
   // byte offsets are 32 bits wide: into a slot's weights and the looked-up rows, and into one slot's rows where they are the contraction
@@ -500,7 +584,7 @@ bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a) {
 }
 
 int launch_tile(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st) {
-  (void)weights;
+  if (weights == kW4) return epilogue == kEpSwiglu ? launch_mapped<kFwd, kEpSwiglu, true>(a, st) : launch_mapped<kFwd, kEpBf16, true>(a, st);
   if (way == kDgrad) {
     if (epilogue == kEpBack) return launch_mapped<kDgrad, kEpBack>(a, st);
     return launch_mapped<kDgrad, kEpBf16>(a, st);
