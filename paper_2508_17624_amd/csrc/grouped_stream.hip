@@ -235,10 +235,12 @@ bool stream_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   const bool mapped = a.g.por != nullptr || a.g.k > 1;
   if (mapped && (unsigned long long)a.x_rows * a.K * 2 >= lim) return false;
   if (a.slot_bytes >= lim) return false;
-  // What the waves of a workgroup can hold of x, and where it is the faster kernel.
+  // What the waves of a workgroup can hold of x, and where it is faster than the tiles: us, 64 slots of 2048 x 1408 with so many rows, this kernel / tiles:
+  // 4 bits, both products: 16 81 / 129, 32 105 / 132, 48 161 / 145; bf16, first product: 4 134 / 141, 12 142 / 143, 24 155 / 146 (weights of
+  // 16 slots, which the memory-side cache holds: 4 33 / 30).  The host knows the average over all slots; those in use have more.
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;
   if (weights == kW4) return a.K <= 64 * kBlock && a.g.rows <= 32 * used;
-  return a.K <= 16 * kBlock && a.g.rows <= 4 * used;
+  return a.K <= 16 * kBlock && a.g.rows <= 6 * used;
 }
 
 int launch_stream(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st) {

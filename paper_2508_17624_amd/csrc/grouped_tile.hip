@@ -78,7 +78,7 @@ struct Cfg {
   static constexpr int PPR = TA / 8, RPI = 64 / PPR;                 // its pieces of 16 bytes; rows of a load instruction
   static constexpr int WPE = TA == 256 ? 1 : 2;                      // waves per SIMD: what LDS has room for
   static_assert(TA == TB && LDS * WPE <= 160 * 1024, "LDS budget of a CU");
-  static constexpr int PARTS = TA / 128;                             // W4: 16-byte pieces of codes of a thread and slab
+  static constexpr int RW = TA / 64;                                 // W4: features of a thread
   // first LDS row, along the contraction, of feature fragment i of half a
   static constexpr int feature_row(int a, int i) { return GATED ? (i < MA / 2 ? 0 : TA / 2) + a * (MA / 2) * 32 + i % (MA / 2) * 32 : (a * MA + i) * 32; }
 };
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
       const int r = along_row(n), piece = (lane & 7) ^ swz<false>(r);
       uint32_t src = (uint32_t)r;
       if constexpr (C::MAPPED) src = r < ch.rows ? (uint32_t)source_row(a.g, ch.first + r) : 0u;
-      ob[n] = r < ch.rows ? (src * (uint32_t)K + piece * 8) * 2 : kNowhere;
+      ob[n] = r < ch.rows ? (src * (uint32_t)K + (C::W4 ? (piece >> 1) * 32 + (piece & 1) * 8 : piece * 8)) * 2 : kNowhere;
     }
     sb = kSlab * 2;
     pb = C::MAPPED ? xp : xp + (size_t)ch.first * K * 2;
@@ -298,48 +298,61 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     for (int n = 0; n < C::NL; ++n)
       if (kt * kSlab + ((lane & 7) ^ swz<decltype(features)::value>(along_row(n))) * 8 >= K) off[n] = kNowhere;
   };
-  // W4: a thread fetches 32 or 16 bytes of codes of one feature two slabs ahead, and turns them into bf16 in LDS a slab ahead of their use.
-  const int w4_row = C::PARTS == 2 ? (int)threadIdx.x : (int)threadIdx.x >> 1, w4_half = C::PARTS == 2 ? 0 : (int)threadIdx.x & 1;
-  uint32_t w4_codes = kNowhere, w4_scales = kNowhere;
-  u32x4 codes[2][C::PARTS];
-  uint32_t scales[2] = {};
+  // W4: codes come two slabs at a time, 64 bytes of a feature by four neighbouring lanes, a lane's 16 bytes being one group of 32 with one
+  // scale.  The even slab of the two takes the first half of every group, the odd one the second (x is loaded to match), so all lanes turn
+  // half of what they hold into bf16 in LDS, a slab ahead of its use.  (A lane with 32 bytes of a feature of its own instead, a slab's worth,
+  // touches 64 lines per load instruction: 64 slots of 16 rows, both products of the FFN, 161 us instead of 147.)
+  u32x4 codes[C::RW], codes_next[C::RW];
+  uint32_t scales[C::RW] = {}, scales_next[C::RW] = {}, w4_codes[C::RW], w4_scales[C::RW];
   if constexpr (C::W4) {
-    const int f = a0 + (C::GATED && w4_row >= C::TA / 2 ? w4_row - C::TA / 2 : w4_row);
-    const uint32_t row = (uint32_t)(C::GATED && w4_row >= C::TA / 2 ? f + N : f);
-    if (f < N) {
-      w4_codes = row * (uint32_t)(K / 2) + 16 * w4_half;
-      w4_scales = (uint32_t)w4_scales_at(C::GATED ? 2 * N : N, K) + row * (uint32_t)(K / 32) + w4_half;
+#pragma unroll
+    for (int i = 0; i < C::RW; ++i) {
+      const int r = wave * (C::TA / 4) + 16 * i + (lane >> 2), f = a0 + (C::GATED && r >= C::TA / 2 ? r - C::TA / 2 : r);
+      const uint32_t row = (uint32_t)(C::GATED && r >= C::TA / 2 ? f + N : f);
+      w4_codes[i] = f < N ? row * (uint32_t)(K / 2) + 16 * (lane & 3) : kNowhere;
+      w4_scales[i] = f < N ? (uint32_t)w4_scales_at(C::GATED ? 2 * N : N, K) + row * (uint32_t)(K / 32) + (lane & 3) : kNowhere;
     }
   }
-  auto fetch = [&](int kt, auto odd) {
+  auto fetch_codes = [&](int two) {
     if constexpr (C::W4) {
-      constexpr int o = decltype(odd)::value;
-      const Rsrc r = resource(pa, kt < nk ? na_bytes : 0u);
+      const Rsrc r = resource(pa, 2 * two < nk ? na_bytes : 0u);
 #pragma unroll
-      for (int p = 0; p < C::PARTS; ++p)
-        codes[o][p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)w4_codes, kt * (kSlab / 2) + 16 * p, 0));
-      if constexpr (C::PARTS == 2) scales[o] = __builtin_amdgcn_raw_buffer_load_b16(r, (int)w4_scales, kt * (kSlab / 32), 0);
-      else scales[o] = __builtin_amdgcn_raw_buffer_load_b8(r, (int)w4_scales, kt * (kSlab / 32), 0);
+      for (int i = 0; i < C::RW; ++i) codes_next[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)w4_codes[i], two * kSlab, 0));
     }
   };
-  auto stage = [&](int unit, int n, auto odd) {  // piece n (of 4 PARTS) of the thread's codes
+  auto fetch_scales = [&](int two) {
     if constexpr (C::W4) {
-      constexpr int o = decltype(odd)::value;
-      const float scale = __uint_as_float((scales[o] >> (8 * (n >> 2)) & 255u) << 23);
-      const uint32_t word = codes[o][C::PARTS == 2 ? n >> 2 : 0][n & 3];
+      const Rsrc r = resource(pa, 2 * two < nk ? na_bytes : 0u);
+#pragma unroll
+      for (int i = 0; i < C::RW; ++i) scales_next[i] = __builtin_amdgcn_raw_buffer_load_b8(r, (int)w4_scales[i], two * (kSlab / 16), 0);
+    }
+  };
+  auto fetched = [&] {
+#pragma unroll
+    for (int i = 0; i < C::RW; ++i) {
+      codes[i] = codes_next[i];
+      scales[i] = scales_next[i];
+    }
+  };
+  auto stage = [&](int unit, int n, auto half_tag) {  // 16 bytes in LDS: word n & 1 of half a group of feature n / 2
+    if constexpr (C::W4) {
+      constexpr int half = decltype(half_tag)::value;
+      const int r = wave * (C::TA / 4) + 16 * (n >> 1) + (lane >> 2);
+      const float scale = __uint_as_float(scales[n >> 1] << 23);
+      const uint32_t word = codes[n >> 1][2 * half + (n & 1)];
       u32x4 v;
       v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
       v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
       v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
       v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
-      const uint32_t at = (uint32_t)(uintptr_t)(lds_byte*)s_lds + unit * C::UNIT + w4_row * 128 + ((4 * w4_half + n) ^ swz<true>(w4_row)) * 16;
+      const uint32_t at = (uint32_t)(uintptr_t)(lds_byte*)s_lds + unit * C::UNIT + r * 128 + ((2 * (lane & 3) + (n & 1)) ^ swz<true>(r)) * 16;
       asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v));
     }
   };
   auto load_a = [&](int kt, int unit, int n) {
     load_lds(resource(pa, kt < nk ? na_bytes : 0u), lds_at(unit, n), C::WAY == kWgrad && C::MAPPED ? step_a[C::WAY == kWgrad ? n : 0] : oa[n], (uint32_t)kt * sa);
   };
-  auto load_b = [&](int kt, int unit, int n) { load_lds(resource(pb, kt < nk ? nb_bytes : 0u), lds_at(unit, n), ob[n], (uint32_t)kt * sb); };
+  auto load_b = [&](int kt, int unit, int n) { load_lds(resource(pb, kt < nk ? nb_bytes : 0u), lds_at(unit, n), ob[n], C::W4 ? (uint32_t)(kt >> 1) * 256 + (kt & 1) * 32 : (uint32_t)kt * sb); };
   // ---- reading
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte*)s_lds;
   const int wa = wave >> 1, wb = wave & 1, h = lane >> 5;
@@ -369,8 +382,8 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   int slab = 0, now = 0;  // unit of slab `now`'s A
   auto unit_of = [&](int ahead) { return slab + ahead >= C::RING ? slab + ahead - C::RING : slab + ahead; };
   if constexpr (C::W4) {
-    fetch(0, std::integral_constant<int, 0>{});
-    fetch(1, std::integral_constant<int, 1>{});
+    fetch_codes(0);
+    fetch_scales(0);
     in_order();
   }
   look_up(0);
@@ -389,11 +402,12 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   if constexpr (!C::A_ACROSS) cut_tail(oa, 1, std::true_type{});
   in_order();
   if constexpr (C::W4) {
+    fetched();
+    fetch_codes(1);
+    fetch_scales(1);
+    in_order();
 #pragma unroll
-    for (int n = 0; n < 4 * C::PARTS; ++n) stage(0, n, std::integral_constant<int, 0>{});
-    in_order();
-    fetch(2, std::integral_constant<int, 0>{});
-    in_order();
+    for (int n = 0; n < C::NL; ++n) stage(0, n, std::integral_constant<int, 0>{});
     wait_lds();
   } else {
 #pragma unroll
@@ -401,7 +415,7 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     in_order();
   }
   auto step = [&](int kt) -> Slab {
-    wait_mem<C::W4 ? C::PARTS + 1 : C::NL>();  // all but A of slab kt + 1 (W4: the codes of slab kt + 2)
+    wait_mem<C::W4 ? C::RW : C::NL>();  // all but A of slab kt + 1
     __builtin_amdgcn_s_barrier();
     if (kt) slab = unit_of(2);
     now = kt;
@@ -409,17 +423,23 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     if constexpr (!C::B_ACROSS) cut_tail(ob, kt + 1, std::false_type{});
     return {(uint32_t)(slab * C::UNIT), (uint32_t)(unit_of(1) * C::UNIT)};
   };
-  auto load = [&](int q, auto odd) {  // B of the next slab, then A of the one behind it (W4: A of the next slab into LDS, and the codes two behind it)
+  auto load = [&](int q, auto odd_tag) {  // B of the next slab, then A of the one behind it (W4: A of the next slab into LDS, and codes two to four slabs ahead)
     if constexpr (C::W4) {
-      using Next = std::integral_constant<int, 1 - decltype(odd)::value>;
+      constexpr int odd = decltype(odd_tag)::value;
+      static_assert(C::NL == 2 * C::RW, "a piece for each of the second half of the instructions");
       if (q < C::NL) {
         load_b(now + 1, unit_of(3), q);
         if (q == C::NL - 1) in_order();
       } else {
-        if (q - C::NL < 4 * C::PARTS) stage(unit_of(2), q - C::NL, Next{});
+        stage(unit_of(2), q - C::NL, std::integral_constant<int, 1 - odd>{});
         if (q == 2 * C::NL - 1) {
           in_order();
-          fetch(now + 3, Next{});
+          if constexpr (odd == 0) {
+            fetched();
+            fetch_codes(now / 2 + 2);
+          } else {
+            fetch_scales(now / 2 + 2);
+          }
           in_order();
         }
       }
@@ -555,11 +575,13 @@ int launch_cfg(const GemmArgs& a, hipStream_t st) {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// The larger tile where a slot has more than 128 rows on average (the weight gradient: wherever the outputs fill it).
+// The larger tile where a slot has many rows on average (the weight gradient: wherever the outputs fill it).  Both sides, us, 64 slots of 2048 x
+// 1408 with so many rows, small / large tile: bf16, first product: 48 154 / 154, 96 171 / 166, 192 237 / 188; 4 bits, both products: 64 146 / 165,
+// 128 188 / 203, 192 297 / 240.
 template <int WAY, int EP, bool MAPPED, bool W4>
 int launch_sized(const GemmArgs& a, hipStream_t st) {
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;
-  const bool large = WAY == kWgrad ? (long long)a.K * a.N > 512 * 512 : a.g.rows > 64 * used && a.N > 128;
+  const bool large = WAY == kWgrad ? (long long)a.K * a.N > 512 * 512 : a.g.rows > (W4 ? 128 : 64) * used && a.N > 128;
   return large ? launch_cfg<WAY, 256, 256, EP, MAPPED, W4>(a, st) : launch_cfg<WAY, 128, 128, EP, MAPPED, W4>(a, st);
 }
 template <int WAY, int EP, bool W4 = false>
