@@ -277,18 +277,18 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   auto lds_at = [&](int unit, int n) { return (lds_byte*)s_lds + (unit * C::UNIT + (wave * C::NL + n) * 1024); };
   // The K loop's loads take no branches.  A slab that does not exist is loaded through a descriptor of no bytes, rows that do not
   // exist from kNowhere: neither costs memory traffic, and the number of loads in flight is always the same.
-  // Rows of the weight gradient's x are looked up a slab ahead of their loads.
-  uint32_t row_next[C::WAY == kWgrad ? C::NL : 1] = {};
-  uint32_t step_a[C::WAY == kWgrad ? C::NL : 1] = {};  // byte offsets of the looked-up rows
-  auto look_up = [&](int kt) {  // slab kt's rows; those asked for before become offsets
-    if constexpr (C::WAY == kWgrad && C::MAPPED) {
+  // Rows of the weight gradient's x are looked up a slab ahead of their loads: a wave's 16 rows of a slab in one load, handed to the lanes
+  // that need them.  (Every lane loading its own rows is half as many load instructions again: dw13 at 49152 rows 769 us instead of KKK.)
+  constexpr bool LOOK_UP = C::WAY == kWgrad && C::MAPPED;
+  uint32_t row_next = 0, step_a[LOOK_UP ? C::NL : 1] = {};  // token rows on their way; byte offsets of the present ones
+  auto look_up = [&](int kt) {                               // slab kt's rows; those asked for before become offsets
+    if constexpr (LOOK_UP) {
+      static_assert(C::NL * C::RPI == 16, "a wave's rows of a slab");
+      const int r = kt * kSlab + wave * 16 + (lane & 15);
+      const uint32_t token = by_k ? __umulhi(row_next, by_k) : row_next, at = r - kSlab < len ? token * ((uint32_t)K * 2) : 0xFFFF0000u;  // (past the end with the offset in the row, which is below 2^16)
 #pragma unroll
-      for (int n = 0; n < C::NL; ++n) {
-        const int r = kt * kSlab + across_row(n);
-        const uint32_t token = by_k ? __umulhi(row_next[n], by_k) : row_next[n];
-        step_a[n] = r - kSlab < len ? oa[n] + token * ((uint32_t)K * 2) : kNowhere;
-        row_next[n] = r < len ? (uint32_t)(a.g.por ? a.g.por[ch.first + r] : ch.first + r) : 0u;
-      }
+      for (int n = 0; n < C::NL; ++n) step_a[n] = oa[n] + (uint32_t)__shfl((int)at, n * C::RPI + lane / C::PPR, 64);
+      row_next = r < len ? (uint32_t)(a.g.por ? a.g.por[ch.first + r] : ch.first + r) : 0u;
     }
   };
   // The last slab of a contraction that 64 does not divide: pieces past its end (rows across it end by their descriptor).
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     }
   };
   auto load_a = [&](int kt, int unit, int n) {
-    load_lds(resource(pa, kt < nk ? na_bytes : 0u), lds_at(unit, n), C::WAY == kWgrad && C::MAPPED ? step_a[C::WAY == kWgrad ? n : 0] : oa[n], (uint32_t)kt * sa);
+    load_lds(resource(pa, kt < nk ? na_bytes : 0u), lds_at(unit, n), LOOK_UP ? step_a[LOOK_UP ? n : 0] : oa[n], (uint32_t)kt * sa);
   };
   auto load_b = [&](int kt, int unit, int n) { load_lds(resource(pb, kt < nk ? nb_bytes : 0u), lds_at(unit, n), ob[n], C::W4 ? (uint32_t)(kt >> 1) * 256 + (kt & 1) * 32 : (uint32_t)kt * sb); };
   // ---- reading
@@ -601,7 +601,7 @@ bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   // byte offsets are 32 bits wide: into a slot's weights and the looked-up rows, and into one slot's rows where they are the contraction
   const unsigned long long x_bytes = (unsigned long long)a.x_rows * a.K * 2, row_bytes = (unsigned long long)a.g.rows * (a.N > a.K ? a.N : a.K) * 2;
   if (mapped && x_bytes >= lim - 65536) return false;
-  if (way == kWgrad) return row_bytes < lim - (unsigned long long)65536 * 64 && (unsigned long long)a.x_rows * a.g.k * a.g.k < lim;
+  if (way == kWgrad) return row_bytes < lim - (unsigned long long)65536 * 64 && (!mapped || (a.K <= 32000 && (unsigned long long)a.x_rows * a.g.k * a.g.k < lim));
   return (unsigned long long)a.slot_bytes + 64ull * a.N * 2 < lim - 65536 && 256ull * a.K * 2 < lim - 65536;
 }
 
