@@ -93,6 +93,11 @@ __device__ __forceinline__ void body(const GemmArgs& a, const RowChunk& ch, int 
   const Rsrc rx = mapped ? resource(a.x, (uint32_t)a.x_rows * (uint32_t)K * 2u)
                          : resource((const unsigned char*)a.x + (size_t)ch.first * K * 2, (uint32_t)ch.rows * (uint32_t)K * 2u);
   const uint32_t scales_at = (uint32_t)w4_scales_at(C::GATED ? 2 * N : N, K);
+  // Uniform offsets stay within the row, and so within their descriptor, also where the lanes' say that there is nothing to load.
+  auto uniform_at = [&](int b, int byte) {
+    const int at = (kb0 + b) * (kBlock * 2) + byte;
+    return b < n_kb && at < 2 * K ? (uint32_t)at : 0u;
+  };
   StripRun<C::WT> w[C::D];
   auto load = [&](int d, int s) {  // strip s of this workgroup; none: zeros, without memory traffic
     const int f = 16 * (s0 + (C::GATED ? s >> 1 : s)) + m;
@@ -101,7 +106,7 @@ __device__ __forceinline__ void body(const GemmArgs& a, const RowChunk& ch, int 
     if constexpr (C::WT == kW4) {
       const uint32_t at = there ? row * (uint32_t)(K / 2) + 16 * q : kNowhere;
 #pragma unroll
-      for (int b = 0; b < C::XB; ++b) w[d].codes[b] = load16(rw, b < n_kb ? at : kNowhere, (uint32_t)(kb0 + b) * (kBlock / 2));
+      for (int b = 0; b < C::XB; ++b) w[d].codes[b] = load16(rw, b < n_kb ? at : kNowhere, b < n_kb ? (uint32_t)(kb0 + b) * (kBlock / 2) : 0u);
       w[d].scales = load16(rw, there ? scales_at + row * (uint32_t)(K / 32) : kNowhere, (uint32_t)kb0 * (kBlock / 32));
     } else {
       const uint32_t at = there && f < N ? (row * (uint32_t)K + 8 * q) * 2 : kNowhere;
@@ -109,7 +114,7 @@ __device__ __forceinline__ void body(const GemmArgs& a, const RowChunk& ch, int 
       for (int b = 0; b < C::XB; ++b)
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj)
-          w[d].blocks[b].w[jj] = load16(rw, b < n_kb && (kb0 + b) * kBlock + 32 * jj + 8 * q < K ? at : kNowhere, (uint32_t)(kb0 + b) * (kBlock * 2) + 64 * jj);
+          w[d].blocks[b].w[jj] = load16(rw, b < n_kb && (kb0 + b) * kBlock + 32 * jj + 8 * q < K ? at : kNowhere, uniform_at(b, 64 * jj));
     }
   };
 #pragma unroll
@@ -126,7 +131,7 @@ __device__ __forceinline__ void body(const GemmArgs& a, const RowChunk& ch, int 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const bool there = b < n_kb && (C::WT == kW4 || (kb0 + b) * kBlock + 32 * j + 8 * q < K);
-        x[t][b][j] = load16(rx, there ? at : kNowhere, (uint32_t)(kb0 + b) * (kBlock * 2) + (C::WT == kW4 ? 16 : 64) * j);
+        x[t][b][j] = load16(rx, there ? at : kNowhere, uniform_at(b, (C::WT == kW4 ? 16 : 64) * j));
       }
   }
   for (int s = 0; s < strips; s += C::R) {

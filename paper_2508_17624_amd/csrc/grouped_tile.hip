@@ -275,10 +275,11 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     nb_bytes = C::MAPPED ? x_bytes : (uint32_t)ch.rows * (uint32_t)K * 2u;
   }
   auto lds_at = [&](int unit, int n) { return (lds_byte*)s_lds + (unit * C::UNIT + (wave * C::NL + n) * 1024); };
-  // The K loop's loads take no branches.  A slab that does not exist is loaded through a descriptor of no bytes, rows that do not
-  // exist from kNowhere: neither costs memory traffic, and the number of loads in flight is always the same.
+  // The K loop's loads take no branches.  A slab that does not exist is loaded through a descriptor of no bytes (the uniform
+  // offsets stay within their descriptors), rows that do not exist from kNowhere: neither costs memory traffic, and the number of loads in
+  // flight is always the same.
   // Rows of the weight gradient's x are looked up a slab ahead of their loads: a wave's 16 rows of a slab in one load, handed to the lanes
-  // that need them.  (Every lane loading its own rows is half as many load instructions again: dw13 at 49152 rows 769 us instead of KKK.)
+  // that need them.  (Every lane loading its own rows is half as many load instructions again: 49152 rows, 2816 x 2048: 769 us instead of 680.)
   constexpr bool LOOK_UP = C::WAY == kWgrad && C::MAPPED;
   uint32_t row_next = 0, step_a[LOOK_UP ? C::NL : 1] = {};  // token rows on their way; byte offsets of the present ones
   auto look_up = [&](int kt) {                               // slab kt's rows; those asked for before become offsets
@@ -316,6 +317,7 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   auto fetch_codes = [&](int two) {
     if constexpr (C::W4) {
       const Rsrc r = resource(pa, 2 * two < nk ? na_bytes : 0u);
+      if (2 * two >= nk) two = 0;
 #pragma unroll
       for (int i = 0; i < C::RW; ++i) codes_next[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)w4_codes[i], two * kSlab, 0));
     }
@@ -323,6 +325,7 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   auto fetch_scales = [&](int two) {
     if constexpr (C::W4) {
       const Rsrc r = resource(pa, 2 * two < nk ? na_bytes : 0u);
+      if (2 * two >= nk) two = 0;
 #pragma unroll
       for (int i = 0; i < C::RW; ++i) scales_next[i] = __builtin_amdgcn_raw_buffer_load_b8(r, (int)w4_scales[i], two * (kSlab / 16), 0);
     }
@@ -350,9 +353,12 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
     }
   };
   auto load_a = [&](int kt, int unit, int n) {
-    load_lds(resource(pa, kt < nk ? na_bytes : 0u), lds_at(unit, n), LOOK_UP ? step_a[LOOK_UP ? n : 0] : oa[n], (uint32_t)kt * sa);
+    load_lds(resource(pa, kt < nk ? na_bytes : 0u), lds_at(unit, n), LOOK_UP ? step_a[LOOK_UP ? n : 0] : oa[n], kt < nk ? (uint32_t)kt * sa : 0u);
   };
-  auto load_b = [&](int kt, int unit, int n) { load_lds(resource(pb, kt < nk ? nb_bytes : 0u), lds_at(unit, n), ob[n], C::W4 ? (uint32_t)(kt >> 1) * 256 + (kt & 1) * 32 : (uint32_t)kt * sb); };
+  auto load_b = [&](int kt, int unit, int n) {
+    const uint32_t at = C::W4 ? (uint32_t)(kt >> 1) * 256 + (kt & 1) * 32 : (uint32_t)kt * sb;
+    load_lds(resource(pb, kt < nk ? nb_bytes : 0u), lds_at(unit, n), ob[n], kt < nk ? at : 0u);
+  };
   // ---- reading
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte*)s_lds;
   const int wa = wave >> 1, wb = wave & 1, h = lane >> 5;
