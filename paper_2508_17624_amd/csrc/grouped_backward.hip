@@ -5,9 +5,9 @@
 //     dg  = da u s (1 + g (1 - s))      du   = da g s
 //     dx  = W1g^T dg + W1u^T du         dW13 = sum_r [dg; du] x^T
 // g and u are computed again: kept from the forward pass they would be 2 I values a row for as long as the layers behind this one run.
-// They stay in fp32 until dg and du are formed, in the epilogue of the product that makes da: of what lies between the products only
-// dg, du and a are rounded to bf16, as operands of the matrix cores.  (With g, u and da in bf16 too the gradients' relative error is 3.5e-3
-// instead of 2.4e-3.)
+// da comes first, in fp32; the product that makes g and u then forms dg, du and a in its epilogue, where a lane holds both of a feature.  Of what
+// lies between the products only dg, du and a are rounded to bf16, as operands of the matrix cores.  (With g, u and da in bf16 too the
+// gradients' relative error is 3.5e-3 instead of 2.4e-3.)
 #include "grouped_gemm.h"
 
 namespace ew {
@@ -99,11 +99,11 @@ int unpermute_back(const T* dout, const T* y, const int32_t* rop, const float* w
   return EW_OK;
 }
 
-// Workspace: g and u [rows, 2I] fp32, dg and du [rows, 2I], a [rows, I].
+// Workspace: da [rows, I] fp32, dg and du [rows, 2I], a [rows, I].
 struct BackScratch { size_t dh, act, all; };
 BackScratch back_scratch(int num_rows, int I, int dtype) {
   const size_t el = dtype == EW_BF16 ? 2 : 4, n = (size_t)num_rows * I;
-  const size_t dh = align_up(n * 8, 256), act = dh + align_up(n * 2 * el, 256);
+  const size_t dh = align_up(n * 4, 256), act = dh + align_up(n * 2 * el, 256);
   return {dh, act, act + align_up(n * el, 256)};
 }
 
@@ -149,13 +149,13 @@ extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype
   ew::GemmArgs a{};
   int rc;
   if (num_rows > 0) {
-    a.g = mapped; a.x = x; a.x_rows = num_tokens; a.w = w13_base; a.out = ws; a.K = H; a.N = 2 * I; a.slot_bytes = (size_t)2 * I * H * el;
-    if ((rc = ew::launch_gemm(ew::kFwd, wt, ew::kEpF32, bf16, a, st))) return rc;
-    a.g = sorted; a.x = dy; a.x_rows = num_rows; a.w = w2_base; a.out = act; a.h = (const float*)ws; a.dh = dh;
-    a.K = H; a.N = I; a.slot_bytes = (size_t)I * H * el;
-    if ((rc = ew::launch_gemm(ew::kDgrad, wt, ew::kEpBack, bf16, a, st))) return rc;
+    a.g = sorted; a.x = dy; a.x_rows = num_rows; a.w = w2_base; a.out = ws; a.K = H; a.N = I; a.slot_bytes = (size_t)I * H * el;
+    if ((rc = ew::launch_gemm(ew::kDgrad, wt, ew::kEpF32, bf16, a, st))) return rc;
+    a.g = mapped; a.x = x; a.x_rows = num_tokens; a.w = w13_base; a.out = act; a.da = (const float*)ws; a.dh = dh;
+    a.slot_bytes = (size_t)2 * I * H * el;
+    if ((rc = ew::launch_gemm(ew::kFwd, wt, ew::kEpBack, bf16, a, st))) return rc;
     if (dx_sorted) {
-      a.x = dh; a.w = w13_base; a.out = dx_sorted; a.K = 2 * I; a.N = H; a.slot_bytes = (size_t)2 * I * H * el;
+      a.g = sorted; a.x = dh; a.x_rows = num_rows; a.out = dx_sorted; a.K = 2 * I; a.N = H;
       if ((rc = ew::launch_gemm(ew::kDgrad, wt, ep, bf16, a, st))) return rc;
     }
   }

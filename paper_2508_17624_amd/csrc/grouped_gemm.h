@@ -15,7 +15,7 @@ struct GemmArgs {
   const void* w;      // weights of slot 0; kWgrad: dy
   void* out;
   size_t slot_bytes;  // of a slot's weights
-  const float* h;     // kEpBack: [rows, 2N] the first product's sums
+  const float* da;    // kEpBack: [rows, N] gradient of the activation
   void* dh;           // kEpBack: [rows, 2N], in the rows' type
   int K, N;           // kWgrad: K is x's width, N is dy's
   int x_rows;
@@ -24,8 +24,8 @@ struct GemmArgs {
 
 // What becomes of a product's sums.
 enum { kEpBf16 = 0, kEpF32 = 1,
-       kEpSwiglu = 2,   // out[r][n] = silu(g) u (bf16), weights [2N, K]: gate rows, then up rows
-       kEpBack = 3 };   // sums are da: out[r][n] = a, dh[r] = [dg, du], from g and u in h (grouped_backward.hip)
+       kEpSwiglu = 2,   // out[r][n] = silu(g) u, weights [2N, K]: gate rows, then up rows
+       kEpBack = 3 };   // the same out, and dh[r] = [dg, du] from da (grouped_backward.hip)
 
 // Bytes of an expert's [N, K] weights in 4 bits: codes [N, K/2], then scales [N, K/32].
 inline size_t w4_bytes(long long N, long long K) { return (size_t)(N * (K / 2) + N * (K / 32)); }

@@ -32,7 +32,7 @@ constexpr int kTile = 64, kStep = 16, kPitch = kTile + 4;
 // TW: type of the elements; float, uint16_t (bf16), or uint8_t for a 4-bit expert's bytes.
 template <int WAY, typename TX, typename TW, int EP>
 __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n) {
-  constexpr bool GATED = EP == kEpSwiglu;  // 32 features: tile index 16 q + 8 s + r is feature 8 q + r of the gate (s = 0) or up rows
+  constexpr bool GATED = EP == kEpSwiglu || EP == kEpBack;  // 32 features: tile index 16 q + 8 s + r is feature 8 q + r of the gate (s = 0) or up rows
   __shared__ float s_a[kStep][kPitch], s_b[kStep][kPitch];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tile = blockIdx.x % tiles_n, unit = blockIdx.x / tiles_n;
@@ -107,7 +107,16 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int o = a0 + (wave & 1) * 16 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
-      if (o < na) put((TX*)a.out + row * N + o, swiglu(acc[8 * (i >> 2) + (i & 3)], acc[8 * (i >> 2) + 4 + (i & 3)]));
+      if (o >= na) continue;
+      const float g = acc[8 * (i >> 2) + (i & 3)], u = acc[8 * (i >> 2) + 4 + (i & 3)];
+      if constexpr (EP == kEpBack) {
+        const SwigluBack v = swiglu_back(g, u, a.da[row * N + o]);
+        put((TX*)a.out + row * N + o, v.a);
+        put((TX*)a.dh + row * 2 * N + o, v.dg);
+        put((TX*)a.dh + row * 2 * N + N + o, v.du);
+      } else {
+        put((TX*)a.out + row * N + o, swiglu(g, u));
+      }
     }
     return;
   }
@@ -116,12 +125,7 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n) {
   for (int i = 0; i < 16; ++i) {
     const int o = a0 + (wave & 1) * 32 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
     if (o >= na) continue;
-    if constexpr (EP == kEpBack) {
-      const SwigluBack v = swiglu_back(a.h[row * 2 * N + o], a.h[row * 2 * N + N + o], acc[i]);
-      put((TX*)a.out + at + o, v.a);
-      put((TX*)a.dh + row * 2 * N + o, v.dg);
-      put((TX*)a.dh + row * 2 * N + N + o, v.du);
-    } else if constexpr (EP == kEpF32) {
+    if constexpr (EP == kEpF32) {
       float* p = (float*)a.out + at + o;
       *p = WAY == kWgrad && a.accumulate ? *p + acc[i] : acc[i];
     } else {
@@ -138,7 +142,7 @@ int launch_any(const GemmArgs& a, hipStream_t st) {
     tiles = (long long)ceil_div(a.K, kTile) * ceil_div(a.N, kTile);
   } else {
     units = max_chunks(a.g.rows, a.g.P, kTile);
-    tiles = ceil_div(a.N, EP == kEpSwiglu ? kTile / 2 : kTile);
+    tiles = ceil_div(a.N, EP == kEpSwiglu || EP == kEpBack ? kTile / 2 : kTile);
   }
   if (units * tiles >= (1ll << 31)) return fail(EW_ERR_UNSUPPORTED, "grouped product: too many output tiles for one launch");
   if (units * tiles == 0) return EW_OK;
@@ -157,10 +161,10 @@ int launch_any_bf16(int epilogue, const GemmArgs& a, hipStream_t st) {
 
 int launch_gemm_any(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st) {
   if (weights == kW4) return epilogue == kEpSwiglu ? launch_any<kFwd, uint16_t, uint8_t, kEpSwiglu>(a, st) : launch_any<kFwd, uint16_t, uint8_t, kEpBf16>(a, st);
-  if (epilogue == kEpBack) return bf16 ? launch_any<kDgrad, uint16_t, uint16_t, kEpBack>(a, st) : launch_any<kDgrad, float, float, kEpBack>(a, st);
+  if (epilogue == kEpBack) return bf16 ? launch_any<kFwd, uint16_t, uint16_t, kEpBack>(a, st) : launch_any<kFwd, float, float, kEpBack>(a, st);
   if (bf16) {
-    if (way == kFwd) return launch_any_bf16<kFwd, uint16_t>(epilogue, a, st);
-    if (way == kDgrad) return launch_any<kDgrad, uint16_t, uint16_t, kEpBf16>(a, st);
+    if (way == kFwd) return launch_any<kFwd, uint16_t, uint16_t, kEpBf16>(a, st);
+    if (way == kDgrad) return launch_any_bf16<kDgrad, uint16_t>(epilogue, a, st);
     return launch_any_bf16<kWgrad, uint16_t>(epilogue, a, st);
   }
   if (way == kFwd) return launch_any<kFwd, float, float, kEpF32>(a, st);

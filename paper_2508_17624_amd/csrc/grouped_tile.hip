@@ -69,7 +69,7 @@ struct Cfg {
   static constexpr bool MAPPED = MAPPED_;                            // rows of x are looked up
   static constexpr bool W4 = W4_;                                    // weights in 4 bits
   static constexpr bool A_ACROSS = WAY != kFwd, B_ACROSS = WAY == kWgrad;
-  static constexpr bool GATED = EP == kEpSwiglu;
+  static constexpr bool GATED = EP == kEpSwiglu || EP == kEpBack;    // weights [2N, K]: a lane holds g and u of a feature
   static constexpr int WAVES = 4, THREADS = 64 * WAVES;        // two halves of the features x two halves of the rows
   static constexpr int MA = TA / 64, MB = TB / 64;                         // a wave's fragments; row fragment f of half b is rows 32 (b + 2 f) ..
   static constexpr int UNIT = TA * kSlab * 2, RING = 5, LDS = RING * UNIT;
@@ -476,22 +476,34 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
       const int b = b0 + 32 * (wb + 2 * f) + (el & 31);
       if (b >= nb) continue;
       const size_t row = C::WAY == kWgrad ? (size_t)unit * N + b : (size_t)(ch.first + b);
-      if constexpr (C::EP == kEpSwiglu) {
+      if constexpr (C::GATED) {
 #pragma unroll
         for (int i = 0; i < C::MA / 2; ++i) {
           const int o = a0 + C::feature_row(wa, i) + 16 * eh;
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
             if (o + 8 * p >= na) continue;
-            u32x4 v;
+            const f32x16 &g = acc[i][f], &u = acc[C::MA / 2 + i][f];
+            if constexpr (C::EP == kEpSwiglu) {
+              u32x4 v;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float r[2];
+              for (int q = 0; q < 4; ++q)
+                v[q] = bf16_pair(swiglu(g[8 * p + 2 * q], u[8 * p + 2 * q]), swiglu(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1]));
+              *(u32x4*)((uint16_t*)a.out + row * row_len + o + 8 * p) = v;
+            } else {
+              const f32x4* dp = (const f32x4*)(a.da + row * N + o + 8 * p);
+              const f32x4 d[2] = {dp[0], dp[1]};
+              u32x4 va, vg, vu;
 #pragma unroll
-              for (int j = 0; j < 2; ++j) r[j] = swiglu(acc[i][f][8 * p + 2 * q + j], acc[C::MA / 2 + i][f][8 * p + 2 * q + j]);
-              v[q] = bf16_pair(r[0], r[1]);
+              for (int q = 0; q < 4; ++q) {
+                const SwigluBack x = swiglu_back(g[8 * p + 2 * q], u[8 * p + 2 * q], d[q >> 1][2 * (q & 1)]);
+                const SwigluBack y = swiglu_back(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1], d[q >> 1][2 * (q & 1) + 1]);
+                va[q] = bf16_pair(x.a, y.a); vg[q] = bf16_pair(x.dg, y.dg); vu[q] = bf16_pair(x.du, y.du);
+              }
+              *(u32x4*)((uint16_t*)a.out + row * N + o + 8 * p) = va;
+              *(u32x4*)((uint16_t*)a.dh + row * 2 * N + o + 8 * p) = vg;
+              *(u32x4*)((uint16_t*)a.dh + row * 2 * N + N + o + 8 * p) = vu;
             }
-            *(u32x4*)((uint16_t*)a.out + row * row_len + o + 8 * p) = v;
           }
         }
         continue;
@@ -518,26 +530,6 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = bf16_pair(acc[i][f][8 * p + 2 * q], acc[i][f][8 * p + 2 * q + 1]);
             *(u32x4*)((uint16_t*)a.out + row * row_len + o + 8 * p) = v;
-          }
-        } else if constexpr (C::EP == kEpBack) {
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            if (o + 8 * p >= na) continue;
-            const float* hp = a.h + row * 2 * N + o + 8 * p;
-            u32x4 va, vg, vu;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float ra[2], rg[2], ru[2];
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const SwigluBack v = swiglu_back(hp[2 * q + j], hp[N + 2 * q + j], acc[i][f][8 * p + 2 * q + j]);
-                ra[j] = v.a; rg[j] = v.dg; ru[j] = v.du;
-              }
-              va[q] = bf16_pair(ra[0], ra[1]); vg[q] = bf16_pair(rg[0], rg[1]); vu[q] = bf16_pair(ru[0], ru[1]);
-            }
-            *(u32x4*)((uint16_t*)a.out + row * N + o + 8 * p) = va;
-            *(u32x4*)((uint16_t*)a.dh + row * 2 * N + o + 8 * p) = vg;
-            *(u32x4*)((uint16_t*)a.dh + row * 2 * N + N + o + 8 * p) = vu;
           }
         }
       }
@@ -601,8 +593,10 @@ bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   const unsigned long long lim = 1ull << 32;
   if (weights == kW4 ? way != kFwd || a.K % 128 || a.N % 16 : weights != kWBf16 || a.K % 8 || a.N % 8) return false;
   if (epilogue == kEpSwiglu && weights != kW4) return false;
+  if (epilogue == kEpBack && (weights == kW4 || way != kFwd)) return false;
+  if (epilogue == kEpF32 && way == kFwd) return false;  // (nobody asks for these)
   if (!aligned16(a.x) || !aligned16(a.w) || !aligned16(a.out)) return false;
-  if (epilogue == kEpBack && (!aligned16(a.h) || !aligned16(a.dh))) return false;
+  if (epilogue == kEpBack && (!aligned16(a.da) || !aligned16(a.dh))) return false;
   const bool mapped = a.g.por != nullptr || a.g.k > 1;
   // byte offsets are 32 bits wide: into a slot's weights and the looked-up rows, and into one slot's rows where they are the contraction
   const unsigned long long x_bytes = (unsigned long long)a.x_rows * a.K * 2, row_bytes = (unsigned long long)a.g.rows * (a.N > a.K ? a.N : a.K) * 2;
@@ -614,11 +608,11 @@ bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a) {
 int launch_tile(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st) {
   if (weights == kW4) return epilogue == kEpSwiglu ? launch_mapped<kFwd, kEpSwiglu, true>(a, st) : launch_mapped<kFwd, kEpBf16, true>(a, st);
   if (way == kDgrad) {
-    if (epilogue == kEpBack) return launch_mapped<kDgrad, kEpBack>(a, st);
+    if (epilogue == kEpF32) return launch_mapped<kDgrad, kEpF32>(a, st);
     return launch_mapped<kDgrad, kEpBf16>(a, st);
   }
   if (way == kWgrad) return epilogue == kEpF32 ? launch_mapped<kWgrad, kEpF32>(a, st) : launch_mapped<kWgrad, kEpBf16>(a, st);
-  if (epilogue == kEpF32) return launch_mapped<kFwd, kEpF32>(a, st);
+  if (epilogue == kEpBack) return launch_mapped<kFwd, kEpBack>(a, st);
   return launch_mapped<kFwd, kEpBf16>(a, st);
 }
 
