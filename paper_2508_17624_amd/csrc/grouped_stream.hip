@@ -162,7 +162,7 @@ __device__ __forceinline__ void body(const GemmArgs& a, const RowChunk& ch, int 
     __syncthreads();
     auto sum = [&](int r, int t) {
       f32x4 v = part[(r * TL + t) * 64 + lane];
-#pragma unroll
+#pragma unroll(C::NW <= 8 ? C::NW : 3)  // (16 partial sums of two strips at once do not fit beside x)
       for (int p = 1; p < C::NW; ++p) v += part[(p * C::R * TL + r * TL + t) * 64 + lane];
       return v;
     };
@@ -244,7 +244,9 @@ bool stream_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   // 4 bits, both products: 16 81 / 129, 32 105 / 132, 48 161 / 145; bf16, first product: 4 134 / 141, 12 142 / 143, 24 155 / 146 (weights of
   // 16 slots, which the memory-side cache holds: 4 33 / 30).  The host knows the average over all slots; those in use have more.
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;
-  if (weights == kW4) return a.K <= 64 * kBlock && a.g.rows <= 32 * used;
+  // Beyond K = 4096 one tile of 16 rows is all that fits beside the partial sums, and 32 rows would read the weights twice: 8192 x 1024, 64
+  // slots: 16 rows 93 / 106, 32 rows 169 / 110 (both products with a hidden size of 8192: 222 / 333 at 16 rows).
+  if (weights == kW4) return a.K <= 64 * kBlock && a.g.rows <= (a.K <= 32 * kBlock ? 32 : 16) * used;
   return a.K <= 16 * kBlock && a.g.rows <= 6 * used;
 }
 

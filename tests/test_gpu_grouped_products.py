@@ -143,6 +143,42 @@ def test_wgrad_keeps_a_slots_infinities_to_itself(ew):
     assert torch.isnan(dw[0]).all() and torch.isnan(dw[2]).all()
 
 
+@pytest.mark.parametrize("K,tokens_more", [(2048, 0), (2048, 100), (1928, 0), (2056, 0)])
+def test_grouped_gemm_few_rows(ew, K, tokens_more):
+    """Around the longest contraction whose few rows the waves hold; with many tokens a workgroup takes two row tiles."""
+    g, counts, k, N = gen(19), [1, 0, 3, 18, 2, 0, 1, 1], 2, 200
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=k, spare=tokens_more)
+    x, w = normal(g, tokens, K), poison(normal(g, len(counts), N, K, std=0.1), counts)
+    y = ew.moe_grouped_gemm(x.cuda(), k, N, len(counts), c.cuda(), off.cuda(), por.cuda(), w.cuda(), num_rows=len(tok))
+    close(y, ref.gemm(x.double()[tok], w.double(), off, True))
+
+
+@pytest.mark.parametrize("shift", ["x", "w", "out"])
+@pytest.mark.parametrize("counts", [[0, 2, 1, 0, 3], [130, 0, 70]], ids=["few", "many"])
+def test_grouped_products_off_16_bytes(ew, counts, shift):
+    """Buffers that begin two bytes past a 16-byte border take the kernel that reads single elements."""
+    g, k, K, N = gen(20), 2, 128, 64
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=k)
+    rows, P = len(tok), len(counts)
+
+    def place(t, moved):
+        buf = torch.zeros(t.numel() + 8, dtype=t.dtype, device="cuda")
+        v = buf[1 if moved else 0:][:t.numel()].view(t.shape)
+        v.copy_(t)
+        return v
+
+    x, w, dy = normal(g, tokens, K), poison(normal(g, P, N, K, std=0.1), counts), normal(g, rows, N)
+    out = place(torch.full((rows, N), 7.0, dtype=torch.bfloat16), shift == "out")
+    ew.moe_grouped_gemm(place(x, shift == "x"), k, N, P, c.cuda(), off.cuda(), por.cuda(), place(w, shift == "w"), out=out, num_rows=rows)
+    close(out, ref.gemm(x.double()[tok], w.double(), off, True), "fwd")
+    dx = place(torch.full((rows, K), 7.0, dtype=torch.bfloat16), shift == "out")
+    ew.moe_grouped_gemm(place(dy, shift == "x"), 1, K, P, c.cuda(), off.cuda(), None, place(w, shift == "w"), transposed=True, out=dx)
+    close(dx, ref.gemm(dy.double(), w.double(), off, True, True), "dgrad")
+    dw = place(torch.full((P, N, K), 7.0, dtype=torch.bfloat16), shift == "out")
+    ew.moe_grouped_gemm_wgrad(place(dy, shift == "w"), place(x, shift == "x"), k, P, c.cuda(), off.cuda(), por.cuda(), dtype=torch.bfloat16, out=dw)
+    close(dw, ref.wgrad(dy.double(), x.double()[tok], off, True)[:2], "wgrad")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_with_infinities_stay_alone(ew, dtype):
     """One token of infinities, one of NaN: their rows only."""
@@ -294,6 +330,23 @@ def test_w4_scales_of_every_size(ew):
     y[:, 1] = 0
     ref_y, b = ref.gemm(x.double(), v, off, True)
     close(y, (ref_y, b + 2.0 ** -126))   # sums below the normal range may be flushed
+
+
+@pytest.mark.parametrize("counts", [FEW, ONE, [0, 20, 16, 0, 32]], ids=["few", "one", "two row tiles"])
+@pytest.mark.parametrize("K", [2048, 2176, 4096, 4224, 8192, 8320])
+def test_w4_long_contractions(ew, K, counts):
+    """Around the lengths at which more waves share a contraction, and past the longest that they hold."""
+    rng, g, k, P, I = np.random.default_rng(5), gen(18), 2, len(counts), 32
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=k)
+    x = normal(g, tokens, K)
+    packed, w = random_w4(rng, P, 144, K, spread=1)
+    packed[torch.tensor(counts) == 0] = 255
+    y = ew.moe_grouped_gemm_w4(x.cuda(), k, 144, P, c.cuda(), off.cuda(), por.cuda(), packed.cuda(), num_rows=len(tok))
+    close(y, ref.gemm(x.double()[tok], w, off, True), "product")
+    p13, w13 = random_w4(rng, P, 2 * I, K, spread=1)
+    p2, w2 = random_w4(rng, P, K, I, spread=1)
+    y = ew.moe_grouped_ffn_w4(x.cuda(), k, I, P, c.cuda(), off.cuda(), por.cuda(), p13.cuda(), p2.cuda(), num_rows=len(tok))
+    close(y, ref.ffn(x.double()[tok], w13, w2, off, True), "FFN")
 
 
 # ------------------------------------------------------------------------------------------------ as they are used
