@@ -403,9 +403,10 @@ int moe_layer_forward(const ew_layer* layer, const void* x, const int32_t* adapt
  * All of them take rows as the permutation leaves them: sorted by slot, slot s with counts[s] rows from row
  * offsets[s] on, row r made from pair pair_of_row[r] (NULL: pair r), that is from token pair / k.
  * num_rows is the room that the row arrays have; offsets[P] <= num_rows rows exist, and rows behind the last
- * one are neither read nor written.  x has num_tokens rows.  A slot without rows is never dereferenced.  Nothing is kept between
- * calls and no call needs scratch of its own unless it takes a workspace; results do not depend on the
- * launch (no atomics), so calls repeat bit for bit, also out of a captured graph.
+ * one are neither read nor written.  x has num_tokens rows.  A slot without rows is never dereferenced.
+ * Outputs and workspaces overlap neither inputs nor each other.  Nothing is kept between calls and no call needs
+ * scratch of its own unless it takes a workspace; results do not depend on the launch (no atomics), so calls
+ * repeat bit for bit, also out of a captured graph.
  * ===================================================================================== */
 
 /* Matrix products grouped by expert (Sec. 2.1: the grouped matrix multiplication), for row r of slot s:
@@ -416,8 +417,8 @@ int moe_layer_forward(const ew_layer* layer, const void* x, const int32_t* adapt
  *   x [dev] dtype [num_tokens, K]; y [dev] dtype [num_rows, N]
  * fp32 accumulation, rounded once into y.  Any K and N; bf16 runs on the bf16 matrix cores where K and N are
  * multiples of 8, x, w_base and y are aligned to 16 bytes and a slot's weights and the rows of x are
- * addressable with 32-bit byte offsets, and in fp32 otherwise.
- * num_rows = 0 is a no-op.  Errors: INVALID_ARG, UNSUPPORTED (a launch of 2^31 workgroups), HIP. */
+ * addressable with 32-bit byte offsets, and as plain fp32 products, much slower, otherwise.
+ * num_rows = 0 is a no-op.  Errors: INVALID_ARG, UNSUPPORTED (2^24 output tiles or more), HIP. */
 int moe_grouped_gemm(const void* x, int dtype, int num_tokens, int num_rows, int k, int K, int N, int P,
                      int transposed, const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
                      const void* w_base, void* y, void* stream);
@@ -427,7 +428,8 @@ int moe_grouped_gemm(const void* x, int dtype, int num_tokens, int num_rows, int
  *   dy [dev] dtype [num_rows, N]; x [dev] dtype [num_tokens, K]
  *   dw [dev] dw_dtype [num_slots, N, K]: EW_F32, or EW_BF16 for bf16 rows (rounded once).  accumulate != 0
  *      adds to what dw holds (EW_F32 only); otherwise slots without rows get zeros.
- * A product w of the second form (transposed != 0) has the same gradient with dy and x exchanged.
+ * A product of the second form (transposed != 0) has the same gradient with dy and x exchanged.  Matrix cores:
+ * as above, the slots' rows addressable with 32-bit byte offsets, and K <= 32000 where rows of x are looked up.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_tokens, int num_rows, int k, int K,
                            int N, int P, const int32_t* counts, const int32_t* offsets, const int32_t* pair_of_row,
@@ -444,7 +446,7 @@ int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_tok
  *   dw13 [dev] dw_dtype [num_slots, 2I, H], dw2 [dev] dw_dtype [num_slots, H, I], either may be NULL;
  *      dw_dtype and accumulate as for moe_grouped_gemm_wgrad
  * g and u are computed again.  bf16: dg, du and a are rounded to bf16 between the products, nothing else is.
- * Any H and I (what runs on the bf16 matrix cores: as moe_grouped_gemm).
+ * Any H, I below 2^30 (what runs on the bf16 matrix cores: as moe_grouped_gemm).
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
 size_t moe_grouped_ffn_backward_workspace_bytes(int num_rows, int I, int dtype);
 int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype, int num_tokens, int num_rows, int k, int H,

@@ -61,36 +61,36 @@ __global__ __launch_bounds__(256) void k_unpermute_back(const T* __restrict__ do
                                                         const float* __restrict__ w, long long pairs, int k, int H, T* __restrict__ dy,
                                                         float* __restrict__ dw) {
   constexpr int W = V ? Vec<T>::N : 1;
-  const long long p = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (p >= pairs) return;
   const int lane = threadIdx.x & 63;
-  const T* d = dout + (size_t)(p / k) * H;
-  const size_t row = (size_t)rop[p] * H;
-  const float wp = w[p];
-  float sum = 0.f;
-  for (int h = lane * W; h < H; h += 64 * W) {
-    float v[W], o[W], f[W];
-    if constexpr (V) Vec<T>::load(d + h, v); else v[0] = Vec<T>::get(d[h]);
-    if (y) {
-      if constexpr (V) Vec<T>::load(y + row + h, f); else f[0] = Vec<T>::get(y[row + h]);
+  for (long long p = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); p < pairs; p += (long long)gridDim.x * 4) {
+    const T* d = dout + (size_t)(p / k) * H;
+    const size_t row = (size_t)rop[p] * H;
+    const float wp = w[p];
+    float sum = 0.f;
+    for (int h = lane * W; h < H; h += 64 * W) {
+      float v[W], o[W], f[W];
+      if constexpr (V) Vec<T>::load(d + h, v); else v[0] = Vec<T>::get(d[h]);
+      if (y) {
+        if constexpr (V) Vec<T>::load(y + row + h, f); else f[0] = Vec<T>::get(y[row + h]);
 #pragma unroll
-      for (int j = 0; j < W; ++j) sum = fmaf(v[j], f[j], sum);
+        for (int j = 0; j < W; ++j) sum = fmaf(v[j], f[j], sum);
+      }
+#pragma unroll
+      for (int j = 0; j < W; ++j) o[j] = wp * v[j];
+      if constexpr (V) Vec<T>::store(dy + row + h, o); else dy[row + h] = Vec<T>::put(o[0]);
     }
+    if (!y) continue;
 #pragma unroll
-    for (int j = 0; j < W; ++j) o[j] = wp * v[j];
-    if constexpr (V) Vec<T>::store(dy + row + h, o); else dy[row + h] = Vec<T>::put(o[0]);
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) dw[p] = sum;
   }
-  if (!y) return;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if (lane == 0) dw[p] = sum;
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 template <typename T>
 int unpermute_back(const T* dout, const T* y, const int32_t* rop, const float* w, long long pairs, int k, int H, T* dy, float* dw, hipStream_t st) {
-  const dim3 grid((unsigned)((pairs + 3) / 4));
+  const dim3 grid((unsigned)((pairs + 3) / 4 < 1 << 22 ? (pairs + 3) / 4 : 1 << 22));  // (a launch has fewer than 2^32 threads)
   if (H % Vec<T>::N == 0 && aligned16(dout) && aligned16(y) && aligned16(dy))
     hipLaunchKernelGGL((k_unpermute_back<T, true>), grid, dim3(256), 0, st, dout, y, rop, w, pairs, k, H, dy, dw);
   else
@@ -122,7 +122,7 @@ extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype
                                         void* ws, size_t ws_bytes, void* stream) {
   using ew::fail;
   const char* who = "moe_grouped_ffn_backward";
-  if (H < 1 || I < 1 || I > (1 << 30)) return fail(EW_ERR_INVALID_ARG, "%s: need H>=1, 1<=I<=2^30 (got %d, %d)", who, H, I);
+  if (H < 1 || I < 1 || I >= (1 << 30)) return fail(EW_ERR_INVALID_ARG, "%s: need H>=1, 1<=I<2^30 (got %d, %d)", who, H, I);
   if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
     return fail(EW_ERR_INVALID_ARG, "%s: weight gradients are float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);

@@ -50,6 +50,11 @@ __device__ __forceinline__ SwigluBack swiglu_back(float g, float u, float da) {
 }
 __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
+// A launch has fewer than 2^32 threads.
+inline int check_grid(long long workgroups, int threads) {
+  return workgroups * threads < (1ll << 32) ? EW_OK : fail(EW_ERR_UNSUPPORTED, "grouped product: %lld output tiles are too many for one launch", workgroups);
+}
+
 // Checks what every call over sorted rows needs; 0 or an error.
 int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets);
 

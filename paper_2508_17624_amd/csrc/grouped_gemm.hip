@@ -144,7 +144,7 @@ int launch_any(const GemmArgs& a, hipStream_t st) {
     units = max_chunks(a.g.rows, a.g.P, kTile);
     tiles = ceil_div(a.N, EP == kEpSwiglu || EP == kEpBack ? kTile / 2 : kTile);
   }
-  if (units * tiles >= (1ll << 31)) return fail(EW_ERR_UNSUPPORTED, "grouped product: too many output tiles for one launch");
+  if (const int rc = check_grid(units * tiles, 256)) return rc;
   if (units * tiles == 0) return EW_OK;
   hipLaunchKernelGGL((k_gemm_any<WAY, TX, TW, EP>), dim3((unsigned)(units * tiles)), dim3(256), 0, st, a, (int)tiles);
   EW_LAUNCH_CHECK("k_gemm_any");

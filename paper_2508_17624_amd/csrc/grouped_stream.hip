@@ -201,7 +201,7 @@ int launch_cfg(const GemmArgs& a, int per_group, hipStream_t st) {
   using C = Cfg<WT, NW, TL, EP, R, D, WPE>;
   const int groups = ceil_div(ceil_div(a.N, 16), per_group);
   const long long units = max_chunks(a.g.rows, a.g.P, 16 * TL) * groups;
-  if (units >= (1ll << 31)) return fail(EW_ERR_UNSUPPORTED, "grouped product: too many output tiles for one launch");
+  if (const int rc = check_grid(units, 64 * NW)) return rc;
   hipLaunchKernelGGL((k_stream<C>), dim3((unsigned)units), dim3(64 * NW), 0, st, a, groups, per_group);
   EW_LAUNCH_CHECK("k_stream");
   return EW_OK;

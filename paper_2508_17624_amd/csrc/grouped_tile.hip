@@ -562,9 +562,8 @@ int launch_cfg(const GemmArgs& a, hipStream_t st) {
     tiles_a = ceil_div(a.N, C::GATED ? TA / 2 : TA);
     units = max_chunks(a.g.rows, a.g.P, TB) * tiles_a;
   }
-  if (units >= (1ll << 31) - 8) return fail(EW_ERR_UNSUPPORTED, "grouped product: too many output tiles for one launch");
+  if (const int rc = check_grid(units + 7, C::THREADS)) return rc;
   if (units == 0) return EW_OK;
-  static_assert(C::LDS <= 160 * 1024, "LDS budget of a CU");
   const uint32_t by_k = a.g.k > 1 ? (uint32_t)(((1ull << 32) + a.g.k - 1) / a.g.k) : 0u;  // n / k = n * by_k >> 32 for n * k < 2^32 (tile_takes)
   hipLaunchKernelGGL((k_tile<C>), dim3((unsigned)((units + 7) / 8 * 8)), dim3(C::THREADS), 0, st, a, tiles_a, (int)units, by_k);
   EW_LAUNCH_CHECK("k_tile");

@@ -169,7 +169,7 @@ extern "C" int moe_grouped_ffn_w4(const void* x, int num_tokens, int num_rows, i
                                   size_t ws_bytes, void* stream) {
   using ew::fail;
   const char* who = "moe_grouped_ffn_w4";
-  if (H < 1 || I < 1 || I > (1 << 30)) return fail(EW_ERR_INVALID_ARG, "%s: need H>=1, 1<=I<=2^30 (got %d, %d)", who, H, I);
+  if (H < 1 || I < 1 || I >= (1 << 30)) return fail(EW_ERR_INVALID_ARG, "%s: need H>=1, 1<=I<2^30 (got %d, %d)", who, H, I);
   if (!moe_w4_expert_bytes(2 * I, H) || !moe_w4_expert_bytes(H, I))
     return fail(EW_ERR_UNSUPPORTED, "%s: H and I must be multiples of 32 and H*I of 512 (H=%d I=%d)", who, H, I);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;

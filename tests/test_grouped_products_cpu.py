@@ -77,6 +77,17 @@ def test_four_bit_calls_refuse_on_the_host():
     assert ffn(ONE, 4, 4, 2, 128, 128, 3, ONE, ONE, None, None, ONE, ONE, ONE, need, None) == INVALID
 
 
+def test_launches_too_large_are_refused():
+    """2^24 tiles of 256 threads are more than a launch can have; 2 I has to fit an int."""
+    many = 2 ** 31 - 1
+    assert gemm(dtype=ew.EW_F32, rows=many, K=7, N=7, k=1) == UNSUPPORTED and b"too many" in ew.lib().ew_last_error()
+    assert gemm(rows=many, K=8, N=8 * 256 * 4, k=1) == UNSUPPORTED
+    assert wgrad(dtype=ew.EW_F32, K=2 ** 18, N=2 ** 18) == UNSUPPORTED
+    assert ew.lib().moe_grouped_gemm_w4(ONE, 4, many, 1, 128, 16 * 64 * 4, 2 ** 30, ONE, ONE, None, ONE, ONE, None) == UNSUPPORTED
+    assert backward(I=2 ** 30) == INVALID
+    assert ew.lib().moe_grouped_ffn_w4(ONE, 4, 4, 2, 128, 2 ** 30, 3, ONE, ONE, None, ONE, ONE, ONE, ONE, 2 ** 40, None) == INVALID
+
+
 def test_bindings_refuse_what_does_not_fit():
     """Tensors on the host, of another type, too small or not contiguous never reach the library."""
     x, c, off = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
