@@ -2,8 +2,11 @@
 //
 // k_gemm_any is the kernel for fp32, and for bf16 and 4-bit sizes that the matrix-core kernels do not take: plain fp32 products
 // and sums on v_mfma_f32_32x32x2_f32 whatever the inputs' type, any sizes, any alignment.  A workgroup makes 64 x 64 outputs, its four
-// waves 32 x 32 each; 16 contraction steps at a time reach LDS contraction-major, so that both operands are read without bank
-// conflicts whichever way they lie in memory.  Outputs of a lane are four neighbours along the contiguous axis.
+// waves 32 x 32 each; 32 contraction steps at a time reach LDS contraction-major, so that both operands are read without bank
+// conflicts whichever way they lie in memory, and the next 32 are loaded meanwhile.  Outputs of a lane are four neighbours along the contiguous axis.
+// Small calls are bound by the latency of those rounds, large ones by the matrix cores' fp32 rate: 4 slots of 2048 rows, 2048 x 2048, takes 620 to 665 us
+// (103 to 111 TFLOP/s; a large library product reaches 140), and an input gradient 256 x 512 of 128 rows 17 us.  With single loads, 16 steps at a time and
+// nothing loaded ahead the same calls took 1120 to 1830 and 27 us.
 #include "grouped_gemm.h"
 
 namespace ew {
@@ -26,14 +29,13 @@ __device__ __forceinline__ float w4_value(uint32_t code, uint32_t scale) {
   return scale == 255 ? __uint_as_float(0x7FC00000u) : v;
 }
 
-constexpr int kTile = 64, kStep = 16, kPitch = kTile + 4;
+constexpr int kTile = 64, kStep = 32, kPitch = kTile + 4;
 
-// Four elements of an operand, fp32: element (o + i, kk) for i < 4 where ALONG_O, otherwise (o, kk + i).
-// TW: type of the elements; float, uint16_t (bf16), or uint8_t for a 4-bit expert's bytes.
-template <int WAY, typename TX, typename TW, int EP>
+// TW: type of the weights' elements (kWgrad: dy's); float, uint16_t (bf16), or uint8_t for a 4-bit expert's bytes.  VEC: 16-byte loads of floats.
+template <int WAY, typename TX, typename TW, int EP, bool VEC>
 __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n) {
   constexpr bool GATED = EP == kEpSwiglu || EP == kEpBack;  // 32 features: tile index 16 q + 8 s + r is feature 8 q + r of the gate (s = 0) or up rows
-  __shared__ float s_a[kStep][kPitch], s_b[kStep][kPitch];
+  __shared__ float s_a[2][kStep][kPitch], s_b[2][kStep][kPitch];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tile = blockIdx.x % tiles_n, unit = blockIdx.x / tiles_n;
   const int K = a.K, N = a.N;
@@ -55,49 +57,67 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n) {
   }
   const TX* x = (const TX*)a.x;
   const unsigned char* ws = (const unsigned char*)a.w + (WAY == kWgrad ? 0 : (size_t)ch.slot * a.slot_bytes);
-  // operand A: weights, or x of the weight gradient; operand B: token rows, or dy
-  auto at_a = [&](int o, int kk) -> float {  // o < na, kk < len
-    if constexpr (WAY == kWgrad) return as_f32(x[(size_t)source_row(a.g, ch.first + kk) * K + o]);
+  // operand A: weights, or x of the weight gradient; operand B: token rows, or dy.  Where element (o, kk), o < na or nb and kk < len, lies:
+  auto a_at = [&](int o, int kk) -> size_t {
+    if constexpr (WAY == kWgrad) return (size_t)source_row(a.g, ch.first + kk) * K + o;
+    else return WAY == kFwd ? (size_t)o * K + kk : (size_t)kk * N + o;
+  };
+  auto a_value = [&](int o, int kk) -> float {
+    if constexpr (WAY == kWgrad) return as_f32(x[a_at(o, kk)]);
     else if constexpr (sizeof(TW) == 1) {
       const uint32_t two = ws[(size_t)o * (K / 2) + kk / 2];
       return w4_value(kk & 1 ? two >> 4 : two & 15, ws[w4_scales_at(GATED ? 2 * N : N, K) + (size_t)o * (K / 32) + kk / 32]);
-    } else return as_f32(((const TW*)ws)[WAY == kFwd ? (size_t)o * K + kk : (size_t)kk * N + o]);
+    } else return as_f32(((const TW*)ws)[a_at(o, kk)]);
   };
   const int row_k = tid >> 2, k_k = (tid & 3) * 4;   // a thread's four elements along the contraction
   const int k_o = tid >> 4, row_o = (tid & 15) * 4;  // and across it
   int src = 0;
   if constexpr (WAY != kWgrad) src = row_k < nb ? source_row(a.g, ch.first + row_k) : 0;
+  constexpr int J = kStep / 16;
+  float va[J][4], vb[J][4];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int ka = k0 + 16 * j + k_k, kc = k0 + 16 * j + k_o;  // along, across
+      const int f = a0 + (GATED ? 8 * (row_k >> 4) + (row_k & 7) : row_k), ff = GATED && (row_k & 8) ? f + N : f;
+      if constexpr (VEC) {
+        const float *w = (const float*)ws, *xf = (const float*)x;
+        const f32x4 zero = {};
+        f32x4 p, q;
+        if constexpr (WAY == kFwd) p = f < na && ka < len ? *(const f32x4*)(w + a_at(ff, ka)) : zero;
+        else p = a0 + row_o < na && kc < len ? *(const f32x4*)((WAY == kWgrad ? xf : w) + a_at(a0 + row_o, kc)) : zero;
+        if constexpr (WAY == kWgrad) q = b0 + row_o < nb && kc < len ? *(const f32x4*)(w + (size_t)(ch.first + kc) * N + b0 + row_o) : zero;
+        else q = row_k < nb && ka < len ? *(const f32x4*)(xf + (size_t)src * K + ka) : zero;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { va[j][i] = p[i]; vb[j][i] = q[i]; }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (WAY == kFwd) va[j][i] = f < na && ka + i < len ? a_value(ff, ka + i) : 0.f;
+          else va[j][i] = a0 + row_o + i < na && kc < len ? a_value(a0 + row_o + i, kc) : 0.f;
+          if constexpr (WAY == kWgrad) vb[j][i] = b0 + row_o + i < nb && kc < len ? as_f32(((const TW*)ws)[(size_t)(ch.first + kc) * N + b0 + row_o + i]) : 0.f;
+          else vb[j][i] = row_k < nb && ka + i < len ? as_f32(x[(size_t)src * K + ka + i]) : 0.f;
+        }
+      }
+    }
+  };
   f32x16 acc = {};
-  for (int k0 = 0; k0 < len; k0 += kStep) {
-    float va[4], vb[4];
+  fetch(0);
+  for (int k0 = 0, buf = 0; k0 < len; k0 += kStep, buf ^= 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (WAY == kFwd) {
-        const int o = a0 + (GATED ? 8 * (row_k >> 4) + (row_k & 7) : row_k), kk = k0 + k_k + i;
-        va[i] = o < na && kk < len ? at_a(GATED && (row_k & 8) ? o + N : o, kk) : 0.f;
-      } else {
-        const int o = a0 + row_o + i, kk = k0 + k_o;
-        va[i] = o < na && kk < len ? at_a(o, kk) : 0.f;
-      }
-      if constexpr (WAY == kWgrad) {
-        const int o = b0 + row_o + i, kk = k0 + k_o;
-        vb[i] = o < nb && kk < len ? as_f32(((const TW*)ws)[(size_t)(ch.first + kk) * N + o]) : 0.f;
-      } else {
-        const int kk = k0 + k_k + i;
-        vb[i] = row_k < nb && kk < len ? as_f32(x[(size_t)src * K + kk]) : 0.f;
+    for (int j = 0; j < J; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (WAY == kFwd) s_a[buf][16 * j + k_k + i][row_k] = va[j][i]; else s_a[buf][16 * j + k_o][row_o + i] = va[j][i];
+        if constexpr (WAY == kWgrad) s_b[buf][16 * j + k_o][row_o + i] = vb[j][i]; else s_b[buf][16 * j + k_k + i][row_k] = vb[j][i];
       }
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (WAY == kFwd) s_a[k_k + i][row_k] = va[i]; else s_a[k_o][row_o + i] = va[i];
-      if constexpr (WAY == kWgrad) s_b[k_o][row_o + i] = vb[i]; else s_b[k_k + i][row_k] = vb[i];
-    }
-    __syncthreads();
+    __syncthreads();  // (one a step: whoever writes a buffer again has met, at the barrier between, all that read it)
+    fetch(k0 + kStep);
 #pragma unroll
     for (int j = 0; j < kStep; j += 2)
-      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(s_a[j + (lane >> 5)][(wave & 1) * 32 + (lane & 31)],
-                                                 s_b[j + (lane >> 5)][(wave >> 1) * 32 + (lane & 31)], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(s_a[buf][j + (lane >> 5)][(wave & 1) * 32 + (lane & 31)],
+                                                 s_b[buf][j + (lane >> 5)][(wave >> 1) * 32 + (lane & 31)], acc, 0, 0, 0);
   }
   // lane l: B element l % 32, A elements 8 (i / 4) + 4 (l / 32) + i % 4
   const int b = b0 + (wave >> 1) * 32 + (lane & 31);
@@ -146,7 +166,9 @@ int launch_any(const GemmArgs& a, hipStream_t st) {
   }
   if (const int rc = check_grid(units * tiles, 256)) return rc;
   if (units * tiles == 0) return EW_OK;
-  hipLaunchKernelGGL((k_gemm_any<WAY, TX, TW, EP>), dim3((unsigned)(units * tiles)), dim3(256), 0, st, a, (int)tiles);
+  const bool vec = sizeof(TX) == 4 && a.K % 4 == 0 && a.N % 4 == 0 && (((uintptr_t)a.x | (uintptr_t)a.w) & 15) == 0;
+  if (vec) hipLaunchKernelGGL((k_gemm_any<WAY, TX, TW, EP, sizeof(TX) == 4>), dim3((unsigned)(units * tiles)), dim3(256), 0, st, a, (int)tiles);
+  else hipLaunchKernelGGL((k_gemm_any<WAY, TX, TW, EP, false>), dim3((unsigned)(units * tiles)), dim3(256), 0, st, a, (int)tiles);
   EW_LAUNCH_CHECK("k_gemm_any");
   return EW_OK;
 }
