@@ -9,7 +9,7 @@
 // operands of the weight gradient).  The first kind is staged as [rows][64] and read 16 bytes a lane; the second as [64][outputs] and read by
 // ds_read_b64_tr_b16, which transposes 4 x 16 elements over 16 lanes on the way: no transposed copy is made in memory.  Both kinds of
 // LDS rows are XOR-swizzled so that the reads of a wave cover all banks.
-// MFMA row m = 8 a + 4 h + b of a feature fragment is feature 16 h + 4 a + b: a lane's 16 sums are neighbours, stored 16 bytes at a time.
+// MFMA row m = 8 a + 4 h + b of a feature fragment is feature 16 h + 4 a + b: a lane's 16 sums are neighbours.
 //
 // Loads go through buffer descriptors: rows and contraction steps past the end read as zeros (a slot's sums never see what lies behind
 // it, NaN or not), and no index, however wrong, reaches memory outside the tensors.
@@ -79,6 +79,9 @@ struct Cfg {
   static constexpr int WPE = TA == 256 ? 1 : 2;                      // waves per SIMD: what LDS has room for
   static_assert(TA == TB && LDS * WPE <= 160 * 1024, "LDS budget of a CU");
   static constexpr int RW = TA / 64;                                 // W4: features of a thread
+  // Results of a wave and row fragment in LDS, on their way out: 32 rows.  (16 bytes more than a row: rows begin at different banks.)
+  static constexpr int OUT_EL = EP == kEpF32 ? 4 : 2, OUT_ROW = (GATED ? MA / 2 : MA) * 32 * OUT_EL, OUT_PITCH = OUT_ROW + 16, OUT_WAVE = 32 * OUT_PITCH;
+  static_assert(WAVES * OUT_WAVE <= LDS, "what the ring leaves when it is done");
   // first LDS row, along the contraction, of feature fragment i of half a
   static constexpr int feature_row(int a, int i) { return GATED ? (i < MA / 2 ? 0 : TA / 2) + a * (MA / 2) * 32 + i % (MA / 2) * 32 : (a * MA + i) * 32; }
 };
@@ -460,78 +463,107 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
       load_a(now + 2, unit_of(4), q - C::NL);
     }
   };
-  const size_t row_len = C::WAY == kWgrad ? K : N;
+  // Results pass through LDS so that whole lines are stored: a lane has 16 neighbours of one row, and stored as they lie every 16 bytes of a wave
+  // are a request of their own (weight gradient of 128 slots of 1536 x 640 in fp32, 125 rows each on average: 198 us instead of 128; a batch
+  // of 8192 x 6 rows through the FFN's backward: 2622 instead of 2482).  A wave uses its own part of what was the ring, one row fragment at a time.
+  const size_t first_row = C::WAY == kWgrad ? (size_t)unit * N : (size_t)ch.first;
+  int el = lane;
+  auto put = [&](int at, u32x4 v) { *(u32x4*)(s_lds + wave * C::OUT_WAVE + (el & 31) * C::OUT_PITCH + at) = v; };  // at: bytes into the row
+  auto store = [&](int f, void* out, size_t row_len, auto add_tag) {  // rows of fragment f; row_len in elements
+    constexpr bool add = decltype(add_tag)::value;
+    constexpr int lanes = C::OUT_ROW / 16, rows = 64 / lanes;
+#pragma unroll 8
+    for (int t = 0; t < 32 / rows; ++t) {
+      const int r = t * rows + el / lanes, piece = el % lanes, b = b0 + 32 * (wb + 2 * f) + r;
+      const int o = a0 + C::feature_row(wa, 0) + piece * (16 / C::OUT_EL);
+      u32x4 v = *(const u32x4*)(s_lds + wave * C::OUT_WAVE + r * C::OUT_PITCH + piece * 16);
+      if (b >= nb || o >= na) continue;
+      unsigned char* p = (unsigned char*)out + ((first_row + b) * row_len + o) * C::OUT_EL;
+      if constexpr (add) v = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, v) + *(const f32x4*)p);
+      *(u32x4*)p = v;
+    }
+  };
   auto body = [&](auto nbf_tag) {  // with this many live row fragments
     constexpr int NBF = decltype(nbf_tag)::value;
     f32x16 acc[C::MA][NBF] = {};
     multiply<C, NBF>(nk, fa, fb, acc, step, load);
-    wait_mem<0>();  // (of slabs that do not exist: nothing may reach LDS once it is another workgroup's)
-    // results: sums e = 0 .. 15 of a fragment are features 16 h + e
-    int el = lane;
+    wait_mem<0>();  // (of slabs that do not exist: nothing may reach LDS once the ring is used otherwise)
+    __builtin_amdgcn_s_barrier();
+    // sums e = 0 .. 15 of a fragment are features 16 h + e
     asm volatile("" : "+v"(el));  // addresses of results are not made ahead of the loop, where there is no room for them
     const int eh = el >> 5;
 #pragma unroll
     for (int f = 0; f < NBF; ++f) {
       __builtin_amdgcn_sched_barrier(0);  // one fragment's addresses at a time: all of them at once do not fit beside the sums
-      const int b = b0 + 32 * (wb + 2 * f) + (el & 31);
-      if (b >= nb) continue;
-      const size_t row = C::WAY == kWgrad ? (size_t)unit * N + b : (size_t)(ch.first + b);
-      if constexpr (C::GATED) {
+      if constexpr (C::EP == kEpBack) {
+        const int b = b0 + 32 * (wb + 2 * f) + (el & 31);
+        u32x4 vg[C::MA / 2][2], vu[C::MA / 2][2];
 #pragma unroll
-        for (int i = 0; i < C::MA / 2; ++i) {
-          const int o = a0 + C::feature_row(wa, i) + 16 * eh;
+        for (int i = 0; i < C::MA / 2; ++i)
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
-            if (o + 8 * p >= na) continue;
-            const f32x16 &g = acc[i][f], &u = acc[C::MA / 2 + i][f];
-            if constexpr (C::EP == kEpSwiglu) {
-              u32x4 v;
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                v[q] = bf16_pair(swiglu(g[8 * p + 2 * q], u[8 * p + 2 * q]), swiglu(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1]));
-              *(u32x4*)((uint16_t*)a.out + row * row_len + o + 8 * p) = v;
-            } else {
-              const f32x4* dp = (const f32x4*)(a.da + row * N + o + 8 * p);
-              const f32x4 d[2] = {dp[0], dp[1]};
-              u32x4 va, vg, vu;
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const SwigluBack x = swiglu_back(g[8 * p + 2 * q], u[8 * p + 2 * q], d[q >> 1][2 * (q & 1)]);
-                const SwigluBack y = swiglu_back(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1], d[q >> 1][2 * (q & 1) + 1]);
-                va[q] = bf16_pair(x.a, y.a); vg[q] = bf16_pair(x.dg, y.dg); vu[q] = bf16_pair(x.du, y.du);
-              }
-              *(u32x4*)((uint16_t*)a.out + row * N + o + 8 * p) = va;
-              *(u32x4*)((uint16_t*)a.dh + row * 2 * N + o + 8 * p) = vg;
-              *(u32x4*)((uint16_t*)a.dh + row * 2 * N + N + o + 8 * p) = vu;
+            const int o = a0 + C::feature_row(wa, i) + 16 * eh + 8 * p;
+            f32x4 d[2] = {};
+            if (b < nb && o < na) {
+              const f32x4* dp = (const f32x4*)(a.da + (first_row + b) * N + o);
+              d[0] = dp[0]; d[1] = dp[1];
             }
-          }
-        }
-        continue;
-      }
+            const f32x16 &g = acc[i][f], &u = acc[C::MA / 2 + i][f];
+            u32x4 va;
 #pragma unroll
-      for (int i = 0; i < C::MA; ++i) {
-        const int o = a0 + C::feature_row(wa, i) + 16 * eh;
-        if constexpr (C::EP == kEpF32) {
-          float* p = (float*)a.out + row * row_len + o;
+            for (int q = 0; q < 4; ++q) {
+              const SwigluBack x = swiglu_back(g[8 * p + 2 * q], u[8 * p + 2 * q], d[q >> 1][2 * (q & 1)]);
+              const SwigluBack y = swiglu_back(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1], d[q >> 1][2 * (q & 1) + 1]);
+              va[q] = bf16_pair(x.a, y.a); vg[i][p][q] = bf16_pair(x.dg, y.dg); vu[i][p][q] = bf16_pair(x.du, y.du);
+            }
+            put(i * 64 + eh * 32 + p * 16, va);
+          }
+        auto put_all = [&](const u32x4 (&v)[C::MA / 2][2]) {
+#pragma unroll
+          for (int i = 0; i < C::MA / 2; ++i)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) put(i * 64 + eh * 32 + p * 16, v[i][p]);
+        };
+        store(f, a.out, N, std::false_type{});
+        put_all(vg);
+        store(f, a.dh, 2 * (size_t)N, std::false_type{});
+        put_all(vu);
+        store(f, (uint16_t*)a.dh + N, 2 * (size_t)N, std::false_type{});
+      } else if constexpr (C::EP == kEpSwiglu) {
+#pragma unroll
+        for (int i = 0; i < C::MA / 2; ++i)
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const f32x16 &g = acc[i][f], &u = acc[C::MA / 2 + i][f];
+            u32x4 v;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              v[q] = bf16_pair(swiglu(g[8 * p + 2 * q], u[8 * p + 2 * q]), swiglu(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1]));
+            put(i * 64 + eh * 32 + p * 16, v);
+          }
+        store(f, a.out, N, std::false_type{});
+      } else if constexpr (C::EP == kEpF32) {
+#pragma unroll
+        for (int i = 0; i < C::MA; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            if (o + 4 * q >= na) continue;
-            f32x4 v;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = acc[i][f][4 * q + j];
-            if (C::WAY == kWgrad && a.accumulate) v += *(const f32x4*)(p + 4 * q);
-            *(f32x4*)(p + 4 * q) = v;
+            const f32x16& e = acc[i][f];
+            const f32x4 v = {e[4 * q], e[4 * q + 1], e[4 * q + 2], e[4 * q + 3]};
+            put(i * 128 + eh * 64 + q * 16, __builtin_bit_cast(u32x4, v));
           }
-        } else if constexpr (C::EP == kEpBf16) {
+        if (C::WAY == kWgrad && a.accumulate) store(f, a.out, K, std::true_type{});
+        else store(f, a.out, C::WAY == kWgrad ? K : N, std::false_type{});
+      } else {
+#pragma unroll
+        for (int i = 0; i < C::MA; ++i)
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
-            if (o + 8 * p >= na) continue;
             u32x4 v;
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = bf16_pair(acc[i][f][8 * p + 2 * q], acc[i][f][8 * p + 2 * q + 1]);
-            *(u32x4*)((uint16_t*)a.out + row * row_len + o + 8 * p) = v;
+            put(i * 64 + eh * 32 + p * 16, v);
           }
-        }
+        store(f, a.out, C::WAY == kWgrad ? K : N, std::false_type{});
       }
     }
   };
@@ -540,6 +572,7 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   if (mine == 0) {
     idle<C>(nk, step, load);
     wait_mem<0>();
+    __builtin_amdgcn_s_barrier();
   } else if (mine == 1) {
     body(std::integral_constant<int, 1>{});
   } else if (C::MB < 3 || mine == 2) {
