@@ -209,19 +209,24 @@ int launch_cfg(const GemmArgs& a, int per_group, hipStream_t st) {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Strips of results for a workgroup: 16, or as many fewer as it takes to have four workgroups a CU, but 4 at least.
+// Strips for a workgroup: 16, or as many fewer as it takes to have four workgroups a CU, but 4 at least; 2 where even those make no more than
+// one a CU and nothing is left but latency.  (us, 2048 x 1408, one row on so many slots, 4 / 2 strips: 4 bits, both products: 1 12.1 / 10.0,
+// 2 12.2 / 10.0, 12 20.8 / 22.6; bf16, first product: 1 11.8 / 8.1.)
 int strips_per_group(const GemmArgs& a, int strips, int most) {
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;
   while (most > 4 && used * strips < 1024ll * most) most /= 2;
-  return most;
+  return used * strips <= 2 * 256 ? 2 : most;
 }
 
 template <int NW, int EP>
 int launch_w4(const GemmArgs& a, hipStream_t st) {
-  constexpr int PAIR = EP == kEpSwiglu ? 2 : 1;
+  constexpr int PAIR = EP == kEpSwiglu ? 2 : 1, WPE = NW == 4 ? 3 : NW / 4;
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;
-  if (NW == 16 || a.g.rows <= 16 * used) return launch_cfg<kW4, NW, 1, EP, 2, NW == 16 ? 1 : 2, NW == 4 ? 3 : NW / 4>(a, strips_per_group(a, PAIR * a.N / 16, 16) / PAIR, st);
-  return launch_cfg<kW4, NW == 16 ? 8 : NW, 2, EP, 2, 2, 2>(a, strips_per_group(a, PAIR * a.N / 16, 16) / PAIR, st);
+  const int strips = PAIR * a.N / 16;
+  if (NW == 16 || a.g.rows <= 16 * used)
+    return launch_cfg<kW4, NW, 1, EP, 2, NW == 16 ? 1 : 2, WPE>(a, strips_per_group(a, strips, 16) / PAIR, st);
+  constexpr int NW2 = NW == 16 ? 8 : NW;  // (never 16 here)
+  return launch_cfg<kW4, NW2, 2, EP, 2, 2, 2>(a, strips_per_group(a, strips, 16) / PAIR, st);
 }
 template <int EP>
 int launch_w4_waves(const GemmArgs& a, hipStream_t st) {
