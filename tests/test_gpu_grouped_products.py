@@ -220,6 +220,34 @@ def test_grouped_ffn_backward(ew, H, I, counts, dtype, out):
         assert (acc[1] - 1 - got[1]).abs().max() <= 2.0 ** -22 * (1 + got[1].abs().max()) and (acc[2] - 1 - got[2]).abs().max() <= 2.0 ** -22 * (1 + got[2].abs().max())
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("H,I", [(640, 264), (264, 1032)])
+def test_many_rows_on_the_large_tiles(ew, H, I, out):
+    """Slots of several row chunks, widths that end inside a tile, in every direction, and the gradients' products of one another."""
+    counts, k, g = [0, 300, 129, 0, 520, 1], 2, gen(21)
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=k)
+    P, rows = len(counts), len(tok)
+    x, dy = normal(g, tokens, H), normal(g, rows, H, std=0.5)
+    w13, w2 = normal(g, P, 2 * I, H, std=H ** -0.5), normal(g, P, H, I, std=I ** -0.5)
+    want = ref.ffn_backward(x.double()[tok], dy.double(), w13.double(), w2.double(), off, True, out == "bf16")
+    got = ew.moe_grouped_ffn_backward(x.cuda(), dy.cuda(), k, I, P, c.cuda(), off.cuda(), por.cuda(), poison(w13, counts).cuda(), poison(w2, counts).cuda(),
+                                      dw_dtype=DT[out])
+    for name, a, b in zip(("dx", "dw13", "dw2"), got, want):
+        close(a, b, name)
+    dh = normal(g, rows, 2 * I)
+    args = (dh.cuda(), x.cuda(), k, P, c.cuda(), off.cuda(), por.cuda())
+    v, b = ref.wgrad(dh.double(), x.double()[tok], off, out == "bf16")
+    close(ew.moe_grouped_gemm_wgrad(*args, dtype=DT[out]), (v, b), "wgrad")
+    if out == "f32":
+        start = torch.randn(v.shape, generator=g)
+        acc = ew.moe_grouped_gemm_wgrad(*args, accumulate=True, out=start.cuda())
+        close(acc, (v + start.double(), b + 2.0 ** -23 * (v.abs() + start.double().abs())), "accumulated")
+    h = ew.moe_grouped_gemm(x.cuda(), k, 2 * I, P, c.cuda(), off.cuda(), por.cuda(), poison(w13, counts).cuda(), num_rows=rows)
+    close(h, ref.gemm(x.double()[tok], w13.double(), off, True), "fwd")
+    dx = ew.moe_grouped_gemm(dh.cuda(), 1, H, P, c.cuda(), off.cuda(), None, poison(w13, counts).cuda(), transposed=True)
+    close(dx, ref.gemm(dh.double(), w13.double(), off, True, True), "dgrad")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,k,H", [(1, 1, 8), (5, 3, 100), (64, 6, 2048), (257, 8, 264), (3, 64, 7)])
 def test_unpermute_backward(ew, T, k, H, dtype):
