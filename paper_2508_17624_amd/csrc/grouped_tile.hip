@@ -472,9 +472,13 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   auto store = [&](int f, void* out, size_t row_len, auto add_tag) {  // rows of fragment f; row_len in elements
     constexpr bool add = decltype(add_tag)::value;
     constexpr int lanes = C::OUT_ROW / 16, rows = 64 / lanes;
+    // Lanes read what others wrote.  A wave's LDS accesses happen in order, so all it takes is that the compiler keeps theirs: it must not know
+    // that a lane reads elsewhere than it wrote.  (A full barrier for the compiler also holds back the loads of da: 690 -> 707 us for one adapter.)
+    int reader = el;
+    asm volatile("" : "+v"(reader));
 #pragma unroll 8
     for (int t = 0; t < 32 / rows; ++t) {
-      const int r = t * rows + el / lanes, piece = el % lanes, b = b0 + 32 * (wb + 2 * f) + r;
+      const int r = t * rows + reader / lanes, piece = reader % lanes, b = b0 + 32 * (wb + 2 * f) + r;
       const int o = a0 + C::feature_row(wa, 0) + piece * (16 / C::OUT_EL);
       u32x4 v = *(const u32x4*)(s_lds + wave * C::OUT_WAVE + r * C::OUT_PITCH + piece * 16);
       if (b >= nb || o >= na) continue;
