@@ -135,12 +135,16 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
-def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
+def _type_code(dtype: torch.dtype) -> int:
+    if dtype == torch.float32:
         return EW_F32
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return EW_BF16
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    return _type_code(t.dtype)
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor | None:
@@ -472,13 +476,14 @@ def moe_grouped_gemm_wgrad(dy, x, k: int, P: int, counts, offsets, pair_of_row, 
     default); accumulate adds to `out` (float32)."""
     if dy.dim() != 2 or not dy.is_contiguous() or dy.dtype != x.dtype or dy.device != x.device:
         raise ValueError("dy must be a contiguous 2-D tensor of x's type and device")
+    dw_code = _type_code(dtype)
     rows, K, N = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0]), x.shape[1], dy.shape[1]
     n = P - first_slot if num_slots is None else num_slots
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     dw = _result("out", out, (max(n, 0), N, K), dtype, x)
     _check(lib().moe_grouped_gemm_wgrad(_ptr(dy), _ptr(x), _dtype_code(x), x.shape[0], rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
-                                        first_slot, n, _dtype_code(dw), int(accumulate), _ptr(dw), _stream()))
+                                        first_slot, n, dw_code, int(accumulate), _ptr(dw), _stream()))
     return dw
 
 
@@ -490,6 +495,7 @@ def moe_grouped_ffn_backward(x, dy, k: int, I: int, P: int, counts, offsets, pai
     and dw2 (float32).  A token's input gradient: moe_unpermute(dx_sorted, row_of_pair, ones)."""
     if dy.dim() != 2 or not dy.is_contiguous() or dy.dtype != x.dtype or dy.device != x.device or dy.shape[1] != x.shape[1]:
         raise ValueError("dy must be a contiguous [rows, H] tensor of x's type and device")
+    dw_code = _type_code(dw_dtype)
     rows, H = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0]), x.shape[1]
     n = P - first_slot if num_slots is None else num_slots
     if accumulate and (dw13 is None or dw2 is None):
@@ -504,8 +510,8 @@ def moe_grouped_ffn_backward(x, dy, k: int, I: int, P: int, counts, offsets, pai
         dw13 = dw2 = None
     ws = _scratch(ws, lib().moe_grouped_ffn_backward_workspace_bytes(rows, I, _dtype_code(x)), x)
     _check(lib().moe_grouped_ffn_backward(_ptr(x), _ptr(dy), _dtype_code(x), x.shape[0], rows, k, H, I, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row),
-                                          _ptr(w13_base), _ptr(w2_base), _ptr(dx), first_slot, n, EW_F32 if dw_dtype == torch.float32 else EW_BF16,
-                                          int(accumulate), _ptr(dw13), _ptr(dw2), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
+                                          _ptr(w13_base), _ptr(w2_base), _ptr(dx), first_slot, n, dw_code, int(accumulate),
+                                          _ptr(dw13), _ptr(dw2), _ptr(ws), ws.numel() if ws is not None else 0, _stream()))
     return dx, dw13, dw2
 
 
