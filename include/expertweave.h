@@ -469,7 +469,8 @@ int moe_unpermute_backward(const void* dout, const void* y_sorted, const int32_t
  * scale 2^(byte - 127) (255: NaN), the OCP Microscaling format.  An expert's [N, K] weights are one run of
  * moe_w4_expert_bytes(N, K) = 17/32 N K bytes: codes [N, K/2], the even element in the low half of a byte, then
  * scales [N, K/32].  That number is also what expert_pool_create is given for a pool of such experts: pages,
- * adapters and the expert map know nothing of the format.  0: sizes that cannot be packed (K % 32, N*K % 512). */
+ * adapters and the expert map know nothing of the format.  The FFN does: moe_grouped_ffn, its planned and shared forms and
+ * moe_layer_forward read experts of dtype, so such a pool goes to the two _w4 products alone.  0: sizes that cannot be packed (K % 32, N*K % 512). */
 size_t moe_w4_expert_bytes(int N, int K);
 
 /* w [dev] dtype [num_experts, N, K] -> out [dev] [num_experts, moe_w4_expert_bytes(N, K)]: the scale is

@@ -161,6 +161,7 @@ class ExpertPool:
         _check(lib().expert_pool_create(C.byref(self._h), device, num_layers, M, N, E_max, w13_bytes, w2_bytes,
                                         page_bytes, prealloc_pages, flags))
         self.L, self.M, self.N, self.E_max, self.P = num_layers, M, N, E_max, M + N * E_max
+        self.w13_bytes, self.w2_bytes = w13_bytes, w2_bytes
         self.flags, self.device = flags, device
         self._keep = []
 

@@ -61,7 +61,8 @@ class LayerBuffers:
 
 
 class MoELayer:
-    """One MoE layer bound to a pool layer."""
+    """One MoE layer bound to a pool layer.  The pool holds experts of the layer's type (float32 or bfloat16); experts in 4 bits are for
+    moe_grouped_ffn_w4 and moe_grouped_gemm_w4, called behind the permutation."""
 
     def __init__(self, pool: B.ExpertPool, layer: int, Wg: torch.Tensor, shared_w13, shared_w2, k: int, I: int,
                  T_max: int, dtype: torch.dtype, bias: torch.Tensor | None = None, renormalize: bool = False,
@@ -71,6 +72,12 @@ class MoELayer:
         self.Wg, self.bias, self.renormalize = Wg, bias, renormalize
         self.w13_base, self.w2_base, self.emap, _ = pool.view(layer)
         self.H = Wg.shape[1]
+        # A layer pass reads experts of its own type, one right behind the other: a pool of another type's experts, or of 4-bit ones, would
+        # be read as noise and past its end.
+        el = torch.empty(0, dtype=dtype).element_size()
+        if (pool.w13_bytes, pool.w2_bytes) != (2 * I * self.H * el, self.H * I * el):
+            raise ValueError(f"the pool's experts have {pool.w13_bytes} + {pool.w2_bytes} bytes, a layer of {dtype}, H={self.H}, I={I} reads "
+                             f"{2 * I * self.H * el} + {self.H * I * el}")
         self.S = 0 if shared_w13 is None else shared_w13.shape[0]
         self.shared_w13, self.shared_w2 = shared_w13, shared_w2
         self.T_max = self._T = T_max

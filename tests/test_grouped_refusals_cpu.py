@@ -27,3 +27,23 @@ def test_weight_gradients_of_other_types_are_refused(dtype):
     out = torch.zeros(3, 64, 64, dtype=dtype)
     with pytest.raises(TypeError, match="unsupported dtype"):
         ew.moe_grouped_gemm_wgrad(dy, x, 1, 3, c, off, None, dtype=dtype, out=out)
+
+
+def test_a_layer_refuses_a_pool_of_other_experts():
+    """A pass over a pool of 4-bit experts would read bf16 weights 3.8 times too far apart, past the end of the pool's range."""
+    from paper_2508_17624_amd.layer import MoELayer, MoEStack
+    M, H, I, k = 4, 64, 32, 2
+    Wg = torch.zeros(M, H)
+    sizes = {"4 bits": (ew.moe_w4_expert_bytes(2 * I, H), ew.moe_w4_expert_bytes(H, I)), "bf16": (2 * I * H * 2, H * I * 2),
+             "f32": (2 * I * H * 4, H * I * 4), "other H": (2 * I * H * 4, H * I * 2)}
+    for name, (b13, b2) in sizes.items():
+        pool = ew.ExpertPool(1, M, 1, 2, b13, b2, flags=ew.EW_POOL_FAKE)
+        for dtype, fits in ((torch.bfloat16, "bf16"), (torch.float32, "f32")):
+            if name == fits:
+                assert MoELayer(pool, 0, Wg, None, None, k, I, 8, dtype).H == H
+                continue
+            with pytest.raises(ValueError, match="bytes"):
+                MoELayer(pool, 0, Wg, None, None, k, I, 8, dtype)
+            with pytest.raises(ValueError, match="bytes"):
+                MoEStack(pool, [Wg], [(None, None)], k, I, 8, dtype)
+        pool.close()
