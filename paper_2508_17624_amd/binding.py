@@ -186,9 +186,11 @@ class ExpertPool:
         if expert_ids is not None:
             ids = (C.c_int32 * len(expert_ids))(*[int(e) for e in expert_ids])
             n = len(expert_ids)
-        for w in (w13, w2):
+        for w, each in ((w13, self.w13_bytes), (w2, self.w2_bytes)):
             if w is not None and not w.is_contiguous():
                 raise ValueError("weights must be contiguous")
+            if w is not None and w.numel() * w.element_size() < n * each:
+                raise ValueError(f"weights have {w.numel() * w.element_size()} bytes, {n} experts of {each} are needed")
         st = stream if stream is not None else (None if self.fake else _stream())
         _check(lib().expert_pool_map(self._h, layer, adapter_id, n, C.cast(ids, C.c_void_p) if ids is not None else None,
                                      _ptr(w13), _ptr(w2), st))

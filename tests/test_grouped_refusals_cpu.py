@@ -47,3 +47,16 @@ def test_a_layer_refuses_a_pool_of_other_experts():
             with pytest.raises(ValueError, match="bytes"):
                 MoEStack(pool, [Wg], [(None, None)], k, I, 8, dtype)
         pool.close()
+
+
+def test_a_pool_refuses_weights_shorter_than_its_experts():
+    """4-bit experts handed to a bf16 pool, or too few of them, would be copied from past the end of the tensor."""
+    M, H, I = 3, 64, 32
+    pool = ew.ExpertPool(1, M, 1, 2, 2 * I * H * 2, H * I * 2, flags=ew.EW_POOL_FAKE)
+    w13, w2 = torch.zeros(M, 2 * I, H, dtype=torch.bfloat16), torch.zeros(M, H, I, dtype=torch.bfloat16)
+    packed = torch.zeros(M, ew.moe_w4_expert_bytes(2 * I, H), dtype=torch.uint8)
+    for a, b in ((packed, w2), (w13[:2], w2), (w13, w2[:2])):
+        with pytest.raises(ValueError, match="bytes"):
+            pool.map(0, 0, list(range(M)), a, b)
+    pool.map(0, 0, list(range(M)), w13, w2)
+    pool.close()
