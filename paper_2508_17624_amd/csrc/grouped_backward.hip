@@ -123,6 +123,7 @@ extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype
   using ew::fail;
   const char* who = "moe_grouped_ffn_backward";
   if (H < 1 || I < 1 || I >= (1 << 30)) return fail(EW_ERR_INVALID_ARG, "%s: need H>=1, 1<=I<2^30 (got %d, %d)", who, H, I);
+  if (const int rc = ew::check_sizes(who, "H", H, "2 I", 2ll * I)) return rc;
   if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
     return fail(EW_ERR_INVALID_ARG, "%s: weight gradients are float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);
@@ -178,6 +179,7 @@ extern "C" int moe_unpermute_backward(const void* dout, const void* y_sorted, co
   using ew::fail;
   const char* who = "moe_unpermute_backward";
   if (T < 0 || k < 1 || H < 1) return fail(EW_ERR_INVALID_ARG, "%s: need T>=0, k>=1, H>=1 (got %d, %d, %d)", who, T, k, H);
+  if (const int rc = ew::check_size(who, "H", H)) return rc;
   if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if ((long long)T * k >= (1ll << 31)) return fail(EW_ERR_UNSUPPORTED, "%s: the row count must be below 2^31", who);
   if (T == 0) return EW_OK;

@@ -50,12 +50,19 @@ __device__ __forceinline__ SwigluBack swiglu_back(float g, float u, float da) {
 }
 __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
+// Loops and tile borders count in 32 bits and reach a little past the ends: sizes and rows stay this far below 2^31.
+constexpr int kMostSize = (int)((1u << 31) - 1024);
+inline int check_size(const char* who, const char* what, long long v) {
+  return v <= kMostSize ? EW_OK : fail(EW_ERR_UNSUPPORTED, "%s: %s=%lld is too many (at most 2^31 - 1024)", who, what, v);
+}
+
 // A launch has fewer than 2^32 threads.
 inline int check_grid(long long workgroups, int threads) {
   return workgroups * threads < (1ll << 32) ? EW_OK : fail(EW_ERR_UNSUPPORTED, "grouped product: %lld output tiles are too many for one launch", workgroups);
 }
 
 // Checks what every call over sorted rows needs; 0 or an error.
+int check_sizes(const char* who, const char* a, long long na, const char* b, long long nb);
 int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets);
 
 }  // namespace ew

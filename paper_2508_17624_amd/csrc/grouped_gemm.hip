@@ -204,7 +204,12 @@ int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, cons
   if (num_tokens < 0 || num_rows < 0 || k < 1 || P < 1)
     return fail(EW_ERR_INVALID_ARG, "%s: need num_tokens>=0, num_rows>=0, k>=1, P>=1 (got %d, %d, %d, %d)", who, num_tokens, num_rows, k, P);
   if (!counts || !offsets) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
-  return EW_OK;
+  return check_size(who, "num_rows", num_rows);
+}
+
+int check_sizes(const char* who, const char* a, long long na, const char* b, long long nb) {
+  const int rc = check_size(who, a, na);
+  return rc ? rc : check_size(who, b, nb);
 }
 
 }  // namespace ew
@@ -215,6 +220,7 @@ extern "C" int moe_grouped_gemm(const void* x, int dtype, int num_tokens, int nu
   using ew::fail;
   const char* who = "moe_grouped_gemm";
   if (K < 1 || N < 1) return fail(EW_ERR_INVALID_ARG, "%s: need K>=1, N>=1 (got %d, %d)", who, K, N);
+  if (const int rc = ew::check_sizes(who, "K", K, "N", N)) return rc;
   if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
   if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
@@ -233,6 +239,7 @@ extern "C" int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, 
   using ew::fail;
   const char* who = "moe_grouped_gemm_wgrad";
   if (K < 1 || N < 1) return fail(EW_ERR_INVALID_ARG, "%s: need K>=1, N>=1 (got %d, %d)", who, K, N);
+  if (const int rc = ew::check_sizes(who, "K", K, "N", N)) return rc;
   if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
     return fail(EW_ERR_INVALID_ARG, "%s: dw is float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);

@@ -151,6 +151,7 @@ extern "C" int moe_grouped_gemm_w4(const void* x, int num_tokens, int num_rows, 
   using ew::fail;
   const char* who = "moe_grouped_gemm_w4";
   if (K < 1 || N < 1) return fail(EW_ERR_INVALID_ARG, "%s: need K>=1, N>=1 (got %d, %d)", who, K, N);
+  if (const int rc = ew::check_sizes(who, "K", K, "N", N)) return rc;
   if (!moe_w4_expert_bytes(N, K)) return fail(EW_ERR_UNSUPPORTED, "%s: K must be a multiple of 32 and N*K of 512 (N=%d K=%d)", who, N, K);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
   if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
@@ -170,6 +171,7 @@ extern "C" int moe_grouped_ffn_w4(const void* x, int num_tokens, int num_rows, i
   using ew::fail;
   const char* who = "moe_grouped_ffn_w4";
   if (H < 1 || I < 1 || I >= (1 << 30)) return fail(EW_ERR_INVALID_ARG, "%s: need H>=1, 1<=I<2^30 (got %d, %d)", who, H, I);
+  if (const int rc = ew::check_sizes(who, "H", H, "2 I", 2ll * I)) return rc;
   if (!moe_w4_expert_bytes(2 * I, H) || !moe_w4_expert_bytes(H, I))
     return fail(EW_ERR_UNSUPPORTED, "%s: H and I must be multiples of 32 and H*I of 512 (H=%d I=%d)", who, H, I);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;

@@ -60,3 +60,33 @@ def test_a_pool_refuses_weights_shorter_than_its_experts():
             pool.map(0, 0, list(range(M)), a, b)
     pool.map(0, 0, list(range(M)), w13, w2)
     pool.close()
+
+
+def test_sizes_whose_loops_would_wrap_are_refused():
+    """A contraction, a width or a slot's rows within a step of 2^31: the index of the step behind the last one has no 32-bit value."""
+    lib, most = ew.lib(), 2 ** 31 - 1024
+    for big in (2 ** 31 - 1, most + 1):
+        for dtype in (ew.EW_F32, ew.EW_BF16):
+            for K, N in ((big, 1), (1, big)):
+                assert lib.moe_grouped_gemm(ONE, dtype, 1, 1, 1, K, N, 1, 0, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
+                assert lib.moe_grouped_gemm_wgrad(ONE, ONE, dtype, 1, 1, 1, K, N, 1, ONE, ONE, ONE, 0, 1, ew.EW_F32, 0, ONE, None) == UNSUPPORTED
+            assert lib.moe_grouped_gemm(ONE, dtype, big, big, 1, 1, 1, 1, 0, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
+            assert lib.moe_grouped_gemm_wgrad(ONE, ONE, dtype, big, big, 1, 1, 1, 1, ONE, ONE, ONE, 0, 1, ew.EW_F32, 0, ONE, None) == UNSUPPORTED
+            for H, I, rows in ((big, 1, 1), (1, 2 ** 30 - 1, 1), (1, 1, big)):
+                assert lib.moe_grouped_ffn_backward(ONE, ONE, dtype, rows, rows, 1, H, I, 1, ONE, ONE, ONE, ONE, ONE, ONE, 0, 1, ew.EW_F32, 0, ONE, ONE, ONE,
+                                                    2 ** 62, None) == UNSUPPORTED
+            assert lib.moe_unpermute_backward(ONE, None, ONE, ONE, 1, 1, big, dtype, ONE, None, None) == UNSUPPORTED
+    big = 2 ** 31 - 512
+    assert lib.moe_grouped_gemm_w4(ONE, 1, 1, 1, big, 1, 1, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
+    assert lib.moe_grouped_ffn_w4(ONE, 1, 1, 1, big, 32, 1, ONE, ONE, ONE, ONE, ONE, ONE, ONE, 2 ** 40, None) == UNSUPPORTED
+    assert b"at most" in lib.ew_last_error()
+
+
+@pytest.mark.parametrize("tokens,rows", [(2 ** 29, 2 ** 27), (2 ** 22 - 1, 2 ** 22 - 1)])
+def test_launches_of_too_many_tiles_are_refused(tokens, rows):
+    """2^24 tiles of 256 threads are more than a launch can have, whatever the sizes themselves are."""
+    lib, wide = ew.lib(), 2 ** 15
+    assert lib.moe_grouped_gemm(ONE, ew.EW_F32, tokens, rows, 1, 7, wide + 1, 4, 0, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
+    assert b"too many for one launch" in lib.ew_last_error()
+    assert lib.moe_grouped_gemm(ONE, ew.EW_BF16, tokens, rows, 1, 8, 64 * wide, 4, 0, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
+    assert b"too many for one launch" in lib.ew_last_error()
