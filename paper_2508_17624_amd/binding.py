@@ -429,12 +429,19 @@ def _current(x):
     return x.device
 
 
-def _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows):
-    """Number of sorted rows of a call, after checking what names them."""
+def _fits(*sizes):
+    """The library counts in 32 bits; a larger number would reach it as another one."""
+    if max(sizes) >= 2 ** 31:
+        raise ValueError(f"sizes and row counts must be below 2^31, got {max(sizes)}")
+
+
+def _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows, width):
+    """Number of sorted rows of a call, after checking what names them; width: its other size."""
     if x.dim() != 2 or not x.is_contiguous():
         raise ValueError("token rows must be a contiguous 2-D tensor")
-    _current(x)
     rows = x.shape[0] * k if num_rows is None else num_rows
+    _fits(*x.shape, rows, k, P, width)
+    _current(x)
     if pair_of_row is None and rows > x.shape[0] * k:
         raise ValueError("more rows than pairs")
     _need("counts", counts, torch.int32, P, x)
@@ -465,7 +472,7 @@ def moe_grouped_gemm(x, k: int, N: int, P: int, counts, offsets, pair_of_row, w_
     """y[r] = W_s x[pair_of_row[r] / k] for the rows r of every slot s, w_base [P, N, K]; transposed: W_s^T, w_base [P, K, N] (the
     input gradient: x = dy, k = 1, pair_of_row None).  w_base: a tensor or a raw device pointer (pool view).
     num_rows defaults to x.shape[0] * k; returns y [num_rows, N], rows behind the last one as they were."""
-    rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
+    rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows, N), x.shape[1]
     _need("w_base", w_base, x.dtype, P * N * K, x)
     y = _result("out", out, (rows, N), x.dtype, x)
     _check(lib().moe_grouped_gemm(_ptr(x), _dtype_code(x), x.shape[0], rows, k, K, N, P, int(transposed), _ptr(counts), _ptr(offsets),
@@ -480,8 +487,9 @@ def moe_grouped_gemm_wgrad(dy, x, k: int, P: int, counts, offsets, pair_of_row, 
     if dy.dim() != 2 or not dy.is_contiguous() or dy.dtype != x.dtype or dy.device != x.device:
         raise ValueError("dy must be a contiguous 2-D tensor of x's type and device")
     dw_code = _type_code(dtype)
-    rows, K, N = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0]), x.shape[1], dy.shape[1]
     n = P - first_slot if num_slots is None else num_slots
+    _fits(abs(first_slot), abs(n))
+    rows, K, N = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0], dy.shape[1]), x.shape[1], dy.shape[1]
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     dw = _result("out", out, (max(n, 0), N, K), dtype, x)
@@ -499,8 +507,9 @@ def moe_grouped_ffn_backward(x, dy, k: int, I: int, P: int, counts, offsets, pai
     if dy.dim() != 2 or not dy.is_contiguous() or dy.dtype != x.dtype or dy.device != x.device or dy.shape[1] != x.shape[1]:
         raise ValueError("dy must be a contiguous [rows, H] tensor of x's type and device")
     dw_code = _type_code(dw_dtype)
-    rows, H = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0]), x.shape[1]
     n = P - first_slot if num_slots is None else num_slots
+    _fits(abs(first_slot), abs(n))
+    rows, H = _sorted_rows(x, k, P, counts, offsets, pair_of_row, dy.shape[0], 2 * I), x.shape[1]
     if accumulate and (dw13 is None or dw2 is None):
         raise ValueError("accumulate needs dw13 and dw2")
     _need("w13_base", w13_base, x.dtype, P * 2 * I * H, x)
@@ -523,8 +532,9 @@ def moe_unpermute_backward(dout, row_of_pair, topk_w, y_sorted=None, out=None, d
     T, k = topk_w.shape
     if dout.dim() != 2 or not dout.is_contiguous() or dout.shape[0] != T:
         raise ValueError("dout must be a contiguous [T, H] tensor")
-    _current(dout)
     H = dout.shape[1]
+    _fits(T * k, H)
+    _current(dout)
     _need("row_of_pair", row_of_pair, torch.int32, T * k, dout)
     _need("topk_w", topk_w, torch.float32, T * k, dout)
     _need("y_sorted", y_sorted, dout.dtype, T * k * H, dout)
@@ -539,6 +549,7 @@ def moe_unpermute_backward(dout, row_of_pair, topk_w, y_sorted=None, out=None, d
 def moe_w4_expert_bytes(N: int, K: int) -> int:
     """Bytes of an expert's [N, K] weights in 4 bits: codes [N, K/2], then scales [N, K/32].  Also the size that ExpertPool takes for
     a pool of such experts.  Raises for sizes that cannot be packed."""
+    _fits(N, K)
     n = lib().moe_w4_expert_bytes(N, K)
     if n == 0:
         raise EWError(-6, f"K must be a multiple of 32 and N*K of 512 (N={N} K={K})")
@@ -549,8 +560,9 @@ def moe_quantize_w4(w, out=None):
     """w [E, N, K] (float32 or bfloat16) -> uint8 [E, moe_w4_expert_bytes(N, K)], what ExpertPool.map takes for a 4-bit pool."""
     if w.dim() != 3 or not w.is_contiguous():
         raise ValueError("w must be a contiguous [experts, N, K] tensor")
-    _current(w)
     E, N, K = w.shape
+    _fits(E, N, K)
+    _current(w)
     o = _result("out", out, (E, moe_w4_expert_bytes(N, K)), torch.uint8, w)
     _check(lib().moe_quantize_w4(_ptr(w), _dtype_code(w), E, N, K, _ptr(o), _stream()))
     return o
@@ -570,7 +582,7 @@ def moe_grouped_gemm_w4(x, k: int, N: int, P: int, counts, offsets, pair_of_row,
     """moe_grouped_gemm with 4-bit experts: w4_base uint8 [P, moe_w4_expert_bytes(N, K)] or a raw device pointer; x bfloat16."""
     if x.dtype != torch.bfloat16:
         raise TypeError(f"token rows of 4-bit experts are bfloat16, not {x.dtype}")
-    rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
+    rows, K = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows, N), x.shape[1]
     _need("w4_base", w4_base, torch.uint8, P * moe_w4_expert_bytes(N, K), x)
     y = _result("out", out, (rows, N), x.dtype, x)
     _check(lib().moe_grouped_gemm_w4(_ptr(x), x.shape[0], rows, k, K, N, P, _ptr(counts), _ptr(offsets), _ptr(pair_of_row), _ptr(w4_base), _ptr(y), _stream()))
@@ -583,7 +595,7 @@ def moe_grouped_ffn_w4(x, k: int, I: int, P: int, counts, offsets, pair_of_row, 
     or raw device pointers (pool views); x bfloat16."""
     if x.dtype != torch.bfloat16:
         raise TypeError(f"token rows of 4-bit experts are bfloat16, not {x.dtype}")
-    rows, H = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows), x.shape[1]
+    rows, H = _sorted_rows(x, k, P, counts, offsets, pair_of_row, num_rows, 2 * I), x.shape[1]
     _need("w13_base", w13_base, torch.uint8, P * moe_w4_expert_bytes(2 * I, H), x)
     _need("w2_base", w2_base, torch.uint8, P * moe_w4_expert_bytes(H, I), x)
     y = _result("out", out, (rows, H), x.dtype, x)

@@ -90,3 +90,21 @@ def test_launches_of_too_many_tiles_are_refused(tokens, rows):
     assert b"too many for one launch" in lib.ew_last_error()
     assert lib.moe_grouped_gemm(ONE, ew.EW_BF16, tokens, rows, 1, 8, 64 * wide, 4, 0, ONE, ONE, ONE, ONE, ONE, None) == UNSUPPORTED
     assert b"too many for one launch" in lib.ew_last_error()
+
+
+def test_bindings_refuse_numbers_that_do_not_fit_32_bits():
+    """ctypes hands the low 32 bits on: 2^32 + 4 rows would run as 4, 2^32 features as none."""
+    x, dy, c, off = rows_on_host()
+    w, big = torch.zeros(3, 16, 64, dtype=torch.bfloat16), 2 ** 32 + 4
+    por = torch.zeros(1, dtype=torch.int32).expand(big)          # no memory behind it
+    wide, many = torch.empty(big, 0), torch.zeros(1, 1).expand(big, 1)
+    for call in (lambda: ew.moe_grouped_gemm(x, 1, 16, 3, c, off, por, w, num_rows=big), lambda: ew.moe_grouped_gemm(x, 1, big, 3, c, off, None, 0),
+                 lambda: ew.moe_grouped_gemm(x, big, 16, 3, c, off, por, w, num_rows=2), lambda: ew.moe_grouped_gemm(x, 1, 16, big, c, off, None, 0),
+                 lambda: ew.moe_grouped_gemm(x, 2 ** 31, 16, 3, c, off, None, w), lambda: ew.moe_grouped_gemm_wgrad(dy, x, 1, big, c, off, None, num_slots=1),
+                 lambda: ew.moe_grouped_ffn_backward(x, dy, 1, big, 3, c, off, None, 0, 0), lambda: ew.moe_grouped_gemm_w4(x, 1, big, 3, c, off, None, 0),
+                 lambda: ew.moe_grouped_ffn_w4(x, 1, 2 ** 30, 3, c, off, None, 0, 0), lambda: ew.moe_unpermute_backward(wide, None, many),
+                 lambda: ew.moe_grouped_gemm_wgrad(dy, x, 1, 3, c, off, None, first_slot=2 ** 32 + 1, num_slots=1),
+                 lambda: ew.moe_grouped_ffn_backward(x, dy, 1, 32, 3, c, off, None, 0, 0, first_slot=1 - 2 ** 32, num_slots=1),
+                 lambda: ew.moe_w4_expert_bytes(big, 128), lambda: ew.moe_w4_expert_bytes(16, 2 ** 32 + 32)):
+        with pytest.raises(ValueError, match="below 2\\^31"):
+            call()
