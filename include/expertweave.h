@@ -401,7 +401,7 @@ int moe_layer_forward(const ew_layer* layer, const void* x, const int32_t* adapt
  * The experts' products one by one, with their gradients, and experts held in 4 bits
  *
  * All of them take rows as the permutation leaves them: sorted by slot, slot s with counts[s] rows from row
- * offsets[s] on, row r made from pair pair_of_row[r] (NULL: pair r), that is from token pair / k.
+ * offsets[s] on, row r made from pair pair_of_row[r] (NULL: pair r, and num_rows <= num_tokens*k), that is from token pair / k.
  * num_rows is the room that the row arrays have; offsets[P] <= num_rows rows exist, and rows behind the last
  * one are neither read nor written.  x has num_tokens rows.  A slot without rows is never dereferenced.  K, N, H, 2 I
  * and num_rows are at most 2^31 - 1024 (UNSUPPORTED).

@@ -128,7 +128,7 @@ extern "C" int moe_grouped_ffn_backward(const void* x, const void* dy, int dtype
   if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
     return fail(EW_ERR_INVALID_ARG, "%s: weight gradients are float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);
   if (accumulate && dw_dtype != EW_F32) return fail(EW_ERR_UNSUPPORTED, "%s: only float32 gradients accumulate", who);
-  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets, pair_of_row)) return rc;
   if (first_slot < 0 || num_slots < 0 || first_slot > P - num_slots)
     return fail(EW_ERR_INVALID_ARG, "%s: slots [%d, %d + %d) outside 0..P=%d", who, first_slot, first_slot, num_slots, P);
   const bool want_w = num_slots > 0 && (dw13 || dw2);

@@ -63,6 +63,6 @@ inline int check_grid(long long workgroups, int threads) {
 
 // Checks what every call over sorted rows needs; 0 or an error.
 int check_sizes(const char* who, const char* a, long long na, const char* b, long long nb);
-int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets);
+int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets, const void* pair_of_row);
 
 }  // namespace ew

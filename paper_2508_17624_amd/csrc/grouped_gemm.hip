@@ -200,11 +200,14 @@ int launch_gemm(int way, int weights, int epilogue, bool bf16, const GemmArgs& a
   return launch_gemm_any(way, weights, epilogue, bf16, a, st);
 }
 
-int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets) {
+int check_rows(const char* who, int num_tokens, int num_rows, int k, int P, const void* counts, const void* offsets, const void* pair_of_row) {
   if (num_tokens < 0 || num_rows < 0 || k < 1 || P < 1)
     return fail(EW_ERR_INVALID_ARG, "%s: need num_tokens>=0, num_rows>=0, k>=1, P>=1 (got %d, %d, %d, %d)", who, num_tokens, num_rows, k, P);
   if (!counts || !offsets) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
-  return check_size(who, "num_rows", num_rows);
+  if (const int rc = check_size(who, "num_rows", num_rows)) return rc;
+  if (!pair_of_row && num_rows > (long long)num_tokens * k)
+    return fail(EW_ERR_INVALID_ARG, "%s: without pair_of_row there are no more rows than pairs (num_rows=%d, num_tokens=%d, k=%d)", who, num_rows, num_tokens, k);
+  return EW_OK;
 }
 
 int check_sizes(const char* who, const char* a, long long na, const char* b, long long nb) {
@@ -223,7 +226,7 @@ extern "C" int moe_grouped_gemm(const void* x, int dtype, int num_tokens, int nu
   if (const int rc = ew::check_sizes(who, "K", K, "N", N)) return rc;
   if (dtype != EW_F32 && dtype != EW_BF16) return fail(EW_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
-  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets, pair_of_row)) return rc;
   if (!x || !w_base || !y) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
   ew::GemmArgs a{};
   a.g = {counts, offsets, pair_of_row, P, num_rows, k};
@@ -244,7 +247,7 @@ extern "C" int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, 
   if (dw_dtype != EW_F32 && !(dw_dtype == EW_BF16 && dtype == EW_BF16))
     return fail(EW_ERR_INVALID_ARG, "%s: dw is float32, or bfloat16 for bfloat16 rows (dw_dtype=%d)", who, dw_dtype);
   if (accumulate && dw_dtype != EW_F32) return fail(EW_ERR_UNSUPPORTED, "%s: only float32 gradients accumulate", who);
-  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets, pair_of_row)) return rc;
   if (first_slot < 0 || num_slots < 0 || first_slot > P - num_slots)
     return fail(EW_ERR_INVALID_ARG, "%s: slots [%d, %d + %d) outside 0..P=%d", who, first_slot, first_slot, num_slots, P);
   if (num_slots == 0) return EW_OK;

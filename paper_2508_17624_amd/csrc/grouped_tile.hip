@@ -11,8 +11,9 @@
 // LDS rows are XOR-swizzled so that the reads of a wave cover all banks.
 // MFMA row m = 8 a + 4 h + b of a feature fragment is feature 16 h + 4 a + b: a lane's 16 sums are neighbours.
 //
-// Loads go through buffer descriptors: rows and contraction steps past the end read as zeros (a slot's sums never see what lies behind
-// it, NaN or not), and no index, however wrong, reaches memory outside the tensors.
+// The operands are loaded through buffer descriptors: rows and contraction steps past the end read as zeros (a slot's sums never see what
+// lies behind it, NaN or not), and no looked-up row, however wrong, is read outside x.  Counts and offsets are taken as they are but for the
+// room of the row arrays, and so is pair_of_row where it is read.
 #include "grouped_gemm.h"
 
 #include <type_traits>

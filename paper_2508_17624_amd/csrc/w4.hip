@@ -154,7 +154,7 @@ extern "C" int moe_grouped_gemm_w4(const void* x, int num_tokens, int num_rows, 
   if (const int rc = ew::check_sizes(who, "K", K, "N", N)) return rc;
   if (!moe_w4_expert_bytes(N, K)) return fail(EW_ERR_UNSUPPORTED, "%s: K must be a multiple of 32 and N*K of 512 (N=%d K=%d)", who, N, K);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
-  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets, pair_of_row)) return rc;
   if (!x || !w4_base || !y) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
   return ew::launch_gemm(ew::kFwd, ew::kW4, ew::kEpBf16, true,
                          w4_args(counts, offsets, pair_of_row, P, num_rows, k, x, num_tokens, w4_base, y, K, N, moe_w4_expert_bytes(N, K)), (hipStream_t)stream);
@@ -175,7 +175,7 @@ extern "C" int moe_grouped_ffn_w4(const void* x, int num_tokens, int num_rows, i
   if (!moe_w4_expert_bytes(2 * I, H) || !moe_w4_expert_bytes(H, I))
     return fail(EW_ERR_UNSUPPORTED, "%s: H and I must be multiples of 32 and H*I of 512 (H=%d I=%d)", who, H, I);
   if (num_rows == 0 && k >= 1 && P >= 1) return EW_OK;
-  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets)) return rc;
+  if (const int rc = ew::check_rows(who, num_tokens, num_rows, k, P, counts, offsets, pair_of_row)) return rc;
   if (!x || !w13_base || !w2_base || !y_sorted) return fail(EW_ERR_INVALID_ARG, "%s: NULL device pointer", who);
   const size_t need = moe_grouped_ffn_w4_workspace_bytes(num_rows, I);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)

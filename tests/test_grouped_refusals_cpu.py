@@ -108,3 +108,17 @@ def test_bindings_refuse_numbers_that_do_not_fit_32_bits():
                  lambda: ew.moe_w4_expert_bytes(big, 128), lambda: ew.moe_w4_expert_bytes(16, 2 ** 32 + 32)):
         with pytest.raises(ValueError, match="below 2\\^31"):
             call()
+
+
+def test_rows_without_a_token_are_refused():
+    """Without pair_of_row row r is pair r: with more rows than pairs the last ones would be read from behind x."""
+    lib = ew.lib()
+    need = lib.moe_grouped_ffn_backward_workspace_bytes(9, 32, ew.EW_BF16)
+    for dtype in (ew.EW_F32, ew.EW_BF16):
+        assert lib.moe_grouped_gemm(ONE, dtype, 4, 9, 2, 32, 16, 3, 0, ONE, ONE, None, ONE, ONE, None) == INVALID
+        assert b"pair_of_row" in lib.ew_last_error()
+        assert lib.moe_grouped_gemm_wgrad(ONE, ONE, dtype, 4, 9, 2, 32, 16, 3, ONE, ONE, None, 0, 3, ew.EW_F32, 0, ONE, None) == INVALID
+        assert lib.moe_grouped_ffn_backward(ONE, ONE, dtype, 4, 9, 2, 32, 32, 3, ONE, ONE, None, ONE, ONE, ONE, 0, 3, ew.EW_F32, 0, ONE, ONE, ONE, 2 * need,
+                                            None) == INVALID
+    assert lib.moe_grouped_gemm_w4(ONE, 4, 9, 2, 32, 16, 3, ONE, ONE, None, ONE, ONE, None) == INVALID
+    assert lib.moe_grouped_ffn_w4(ONE, 4, 9, 2, 32, 32, 3, ONE, ONE, None, ONE, ONE, ONE, ONE, 2 ** 20, None) == INVALID
