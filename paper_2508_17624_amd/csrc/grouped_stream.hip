@@ -239,7 +239,7 @@ int launch_w4_waves(const GemmArgs& a, hipStream_t st) {
 
 bool stream_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   const unsigned long long lim = (1ull << 32) - 65536;
-  if (way != kFwd || (weights != kWBf16 && weights != kW4) || (epilogue != kEpBf16 && epilogue != kEpSwiglu)) return false;
+  if (way != kFwd || !(weights == kW4 ? epilogue == kEpBf16 || epilogue == kEpSwiglu : weights == kWBf16 && epilogue == kEpBf16)) return false;
   if (!aligned16(a.x) || !aligned16(a.w) || !aligned16(a.out) || a.N % 8) return false;
   if (weights == kW4 ? a.K % kBlock || a.N % 16 : a.K % 8) return false;
   const bool mapped = a.g.por != nullptr || a.g.k > 1;

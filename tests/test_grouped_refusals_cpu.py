@@ -122,3 +122,40 @@ def test_rows_without_a_token_are_refused():
                                             None) == INVALID
     assert lib.moe_grouped_gemm_w4(ONE, 4, 9, 2, 32, 16, 3, ONE, ONE, None, ONE, ONE, None) == INVALID
     assert lib.moe_grouped_ffn_w4(ONE, 4, 9, 2, 32, 32, 3, ONE, ONE, None, ONE, ONE, ONE, ONE, 2 ** 20, None) == INVALID
+
+
+def test_kernels_take_only_the_forms_that_they_have(tmp_path):
+    """The choice of a kernel asks each whether it takes a product: direction, weights, and what becomes of the sums.  Sizes that suit
+    every kernel, few rows."""
+    import os
+    import shutil
+    import subprocess
+    hipcc = "/opt/rocm/bin/hipcc" if os.path.exists("/opt/rocm/bin/hipcc") else shutil.which("hipcc")
+    if not hipcc:
+        pytest.skip("no hipcc")
+    pkg = os.path.dirname(ew.__file__)
+    src, exe = tmp_path / "forms.cpp", tmp_path / "forms"
+    src.write_text('''#include "grouped_gemm.h"
+int main() {
+  ew::GemmArgs a{};
+  void* p = (void*)256;
+  a.g = {(int32_t*)p, (int32_t*)p, nullptr, 64, 64, 1};
+  a.x = a.w = a.out = a.dh = p; a.da = (float*)p;
+  a.K = a.N = 512; a.x_rows = 64; a.num_slots = 64; a.slot_bytes = 512 * 512 * 2;
+  for (int way = 0; way < 3; ++way)
+    for (int w = 0; w < 3; ++w)
+      for (int ep = 0; ep < 4; ++ep) std::printf("%d %d %d %d %d\\n", way, w, ep, ew::stream_takes(way, w, ep, a), ew::tile_takes(way, w, ep, a));
+}
+''')
+    subprocess.run([hipcc, "-x", "hip", "--offload-host-only", "-std=c++17", "-O0", "-I", os.path.join(pkg, "csrc"), "-I", os.path.join(os.path.dirname(pkg), "include"),
+                    "-c", str(src), "-o", str(tmp_path / "forms.o")], check=True, timeout=100, capture_output=True)
+    subprocess.run([hipcc, str(tmp_path / "forms.o"), os.path.join(pkg, "libexpertweave.so"), "-Wl,-rpath," + pkg, "-o", str(exe)], check=True, timeout=100,
+                   capture_output=True)
+    rows = [tuple(map(int, line.split())) for line in subprocess.run([str(exe)], check=True, capture_output=True, text=True, timeout=60).stdout.splitlines()]
+    fwd, dgrad, wgrad = 0, 1, 2
+    bf16, w4 = 1, 2
+    to_bf16, to_f32, swiglu, back = 0, 1, 2, 3
+    assert len(rows) == 36
+    assert {r[:3] for r in rows if r[3]} == {(fwd, bf16, to_bf16), (fwd, w4, to_bf16), (fwd, w4, swiglu)}
+    assert {r[:3] for r in rows if r[4]} == {(fwd, bf16, to_bf16), (fwd, bf16, back), (dgrad, bf16, to_bf16), (dgrad, bf16, to_f32), (wgrad, bf16, to_bf16),
+                                             (wgrad, bf16, to_f32), (fwd, w4, to_bf16), (fwd, w4, swiglu)}
