@@ -43,11 +43,15 @@ int launch_tile(int way, int weights, int epilogue, const GemmArgs& a, hipStream
 int launch_gemm(int way, int weights, int epilogue, bool bf16, const GemmArgs& a, hipStream_t st);
 
 // a = silu(g) u, and from da the gradients of g and u (kEpBack).
+// The relative error of __expf grows with its argument, to 7e-6 at 80.  That is nothing beside the rounding to bf16 that follows (4e-3);
+// results in fp32 take expf, as the forward pass in fp32 does.
 struct SwigluBack { float a, dg, du; };
+template <bool F32>
 __device__ __forceinline__ SwigluBack swiglu_back(float g, float u, float da) {
-  const float s = 1.f / (1.f + __expf(-g)), gs = g * s;
+  const float s = 1.f / (1.f + (F32 ? expf(-g) : __expf(-g))), gs = g * s;
   return {gs * u, da * u * (s + gs * (1.f - s)), da * gs};
 }
+// (for results in bf16)
 __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
 // Loops and tile borders count in 32 bits and reach a little past the ends: sizes and rows stay this far below 2^31.

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void k_gemm_any(GemmArgs a, int tiles_n) {
       if (o >= na) continue;
       const float g = acc[8 * (i >> 2) + (i & 3)], u = acc[8 * (i >> 2) + 4 + (i & 3)];
       if constexpr (EP == kEpBack) {
-        const SwigluBack v = swiglu_back(g, u, a.da[row * N + o]);
+        const SwigluBack v = swiglu_back<sizeof(TX) == 4>(g, u, a.da[row * N + o]);
         put((TX*)a.out + row * N + o, v.a);
         put((TX*)a.dh + row * 2 * N + o, v.dg);
         put((TX*)a.dh + row * 2 * N + N + o, v.du);

@@ -517,8 +517,8 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
             u32x4 va;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              const SwigluBack x = swiglu_back(g[8 * p + 2 * q], u[8 * p + 2 * q], d[q >> 1][2 * (q & 1)]);
-              const SwigluBack y = swiglu_back(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1], d[q >> 1][2 * (q & 1) + 1]);
+              const SwigluBack x = swiglu_back<false>(g[8 * p + 2 * q], u[8 * p + 2 * q], d[q >> 1][2 * (q & 1)]);
+              const SwigluBack y = swiglu_back<false>(g[8 * p + 2 * q + 1], u[8 * p + 2 * q + 1], d[q >> 1][2 * (q & 1) + 1]);
               va[q] = bf16_pair(x.a, y.a); vg[i][p][q] = bf16_pair(x.dg, y.dg); vu[i][p][q] = bf16_pair(x.du, y.du);
             }
             put(i * 64 + eh * 32 + p * 16, va);
