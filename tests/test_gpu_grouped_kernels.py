@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import grouped_bounds as bounds
 import grouped_ref as ref
 import test_gpu_grouped_products as products
 
@@ -44,3 +45,19 @@ def test_fp32_swiglu_gradients_of_large_gates(ew, H, I):
     close(d2[0, 0], (gs * u, 6 * e * (gs * u).abs()), "a")
     close(d13[0, I:, 0], (da * gs, 6 * e * (da * gs).abs()), "du")
     close(d13[0, :I, 0], (da * u * phi, (da * u).abs() * e_phi), "dg")
+
+
+@pytest.mark.parametrize("H,I,counts", [(264, 72, products.RAGGED), (640, 264, [0, 300, 129, 0, 1, 1])], ids=["small tiles", "large tiles"])
+def test_ffn_gradients_round_dg_du_and_a_alone(ew, H, I, counts):
+    """bf16: dg, du and a are rounded between the products and nothing else is.  Element by element, and in the relative error of the weight
+    gradients in fp32, which then comes from one rounding: a half step of 2^-8 at most, uniform, is 2^-8 / sqrt(3) in the mean square."""
+    g, k, P = gen(41), 2, len(counts)
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=k)
+    x, dy = normal(g, tokens, H), normal(g, len(tok), H, std=0.5)
+    w13, w2 = normal(g, P, 2 * I, H, std=H ** -0.5), normal(g, P, H, I, std=I ** -0.5)
+    got = ew.moe_grouped_ffn_backward(x.cuda(), dy.cuda(), k, I, P, c.cuda(), off.cuda(), por.cuda(), w13.cuda(), w2.cuda())
+    want = bounds.ffn_backward(x.double()[tok], dy.double(), w13.double(), w2.double(), off, True, False)
+    for name, a, b in zip(("dx", "dw13", "dw2"), got, want):
+        close(a, b, name)
+    for name, a, (v, _) in zip(("dw13", "dw2"), got[1:], want[1:]):
+        assert float((a.cpu().double() - v).norm() / v.norm()) <= bounds.ONE_ROUNDING_RMS, name
