@@ -61,3 +61,61 @@ def test_ffn_gradients_round_dg_du_and_a_alone(ew, H, I, counts):
         close(a, b, name)
     for name, a, (v, _) in zip(("dw13", "dw2"), got[1:], want[1:]):
         assert float((a.cpu().double() - v).norm() / v.norm()) <= bounds.ONE_ROUNDING_RMS, name
+
+
+# ------------------------------------------------------------------------------------------------ rows that reach each kernel
+TWO_TILES = [0, 40, 31, 0, 33, 16]   # 20 rows a slot on average, slots of one, two and three tiles of 16 rows
+
+
+@pytest.mark.parametrize("K", [128, 2048, 2176, 4096])
+def test_four_bit_product_of_two_row_tiles(ew, K):
+    """16 to 32 rows a slot on average and up to 4096 elements: workgroups of 4 and of 8 waves with two tiles of rows."""
+    rng, g, k, P, N = np.random.default_rng(42), gen(42), 3, len(TWO_TILES), 144
+    packed, w = products.random_w4(rng, P, N, K)
+    packed[torch.tensor(TWO_TILES) == 0] = 255
+    for shuffled in (True, False):
+        c, off, por, tok, tokens = ref.rows_of(TWO_TILES, g, k=k if shuffled else 1, shuffled=shuffled)
+        x = normal(g, tokens, K)
+        out = torch.full((len(tok) + 3, N), 7.0, dtype=torch.bfloat16, device="cuda")
+        if shuffled:
+            por = torch.cat([por, torch.full((3,), 2 ** 30, dtype=torch.int32)])
+            ew.moe_grouped_gemm_w4(x.cuda(), k, N, P, c.cuda(), off.cuda(), por.cuda(), packed.cuda(), out=out, num_rows=len(tok) + 3)
+        else:
+            ew.moe_grouped_gemm_w4(x.cuda(), 1, N, P, c.cuda(), off.cuda(), None, packed.cuda(), out=out)
+        close(out[:len(tok)], ref.gemm(x.double()[tok], w, off, True))
+        assert (out[len(tok):] == 7.0).all()
+
+
+@pytest.mark.parametrize("H,I", [(128, 128), (2048, 128), (2176, 128), (4096, 128), (128, 2176)])
+def test_four_bit_ffn_of_two_row_tiles(ew, H, I):
+    rng, g, k, P = np.random.default_rng(43), gen(43), 2, len(TWO_TILES)
+    p13, w13 = products.random_w4(rng, P, 2 * I, H, spread=1)
+    p2, w2 = products.random_w4(rng, P, H, I, spread=1)
+    c, off, por, tok, tokens = ref.rows_of(TWO_TILES, g, k=k)
+    x = normal(g, tokens, H)
+    y = ew.moe_grouped_ffn_w4(x.cuda(), k, I, P, c.cuda(), off.cuda(), por.cuda(), p13.cuda(), p2.cuda(), num_rows=len(tok))
+    close(y, ref.ffn(x.double()[tok], w13, w2, off, True))
+
+
+@pytest.mark.parametrize("K,N", [(200, 72), (136, 128), (72, 264), (640, 384)])
+def test_many_rows_that_are_not_looked_up(ew, K, N):
+    """The bf16 tiles, 128 and 256 wide, on rows that lie as they are used."""
+    products.run_gemm(ew, products.RAGGED, K, N, "fwd", "bf16", 1, False, 44)
+
+
+def test_four_bit_tiles_keep_scales_of_255_to_their_feature(ew):
+    """As the few-row kernels: one output is NaN in every row, the others are as without it."""
+    K, N, counts = 128, 32, [300, 0, 90]
+    rng, g = np.random.default_rng(45), gen(45)
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=1)
+    codes = rng.integers(0, 16, (3, N, K)).astype(np.uint8)
+    scales = rng.integers(100, 140, (3, N, K // 32)).astype(np.uint8)
+    x = normal(g, tokens, K)
+    v = torch.from_numpy(ref.values_w4(codes, scales))
+    scales[0, 3, 1], scales[2, 31, 3] = 255, 255
+    y = ew.moe_grouped_gemm_w4(x.cuda(), 1, N, 3, c.cuda(), off.cuda(), por.cuda(), torch.from_numpy(ref.pack_w4(codes, scales)).cuda()).cpu()
+    assert torch.isnan(y[:300, 3]).all() and torch.isnan(y[300:, 31]).all() and int(torch.isnan(y).sum()) == 390
+    value, bound = ref.gemm(x.double()[tok], v, off, True)
+    hit = torch.isnan(y)
+    y[hit], value[hit] = 0, 0
+    close(y, (value, bound))
