@@ -119,3 +119,25 @@ def test_four_bit_tiles_keep_scales_of_255_to_their_feature(ew):
     hit = torch.isnan(y)
     y[hit], value[hit] = 0, 0
     close(y, (value, bound))
+
+
+# ------------------------------------------------------------------------------------------------ places, exchanged operands
+@pytest.mark.parametrize("counts", [[0, 2, 1, 3, 0, 1], [5, 40, 0, 300, 17, 64]], ids=["few", "many"])
+@pytest.mark.parametrize("K,N,dtype", [(256, 144, "bf16"), (640, 384, "bf16"), (36, 100, "bf16"), (36, 100, "f32")])
+def test_a_rows_bits_do_not_depend_on_its_place(ew, K, N, dtype, counts):
+    """The same rows in the opposite order inside their slots, the slots in the opposite order: the same bits."""
+    g, P = gen(46), len(counts)
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=1, shuffled=False)
+    x, wf, wb = normal(g, tokens, K, dtype=dtype).cuda(), normal(g, P, N, K, std=0.1, dtype=dtype).cuda(), normal(g, P, K, N, std=0.1, dtype=dtype).cuda()
+    back = torch.arange(tokens - 1, -1, -1)
+    c2 = c.flip(0).contiguous()
+    off2 = torch.cat([torch.zeros(1, dtype=torch.int32), c2.cumsum(0, dtype=torch.int32)])
+    for w, transposed in ((wf, False), (wb, True)):
+        y = ew.moe_grouped_gemm(x, 1, N, P, c.cuda(), off.cuda(), por.cuda(), w, transposed=transposed)
+        y2 = ew.moe_grouped_gemm(x, 1, N, P, c2.cuda(), off2.cuda(), back.to(torch.int32).cuda(), w.flip(0).contiguous(), transposed=transposed)
+        assert torch.equal(y2.flip(0), y)
+    if K % 128 == 0 and dtype == "bf16":
+        packed = ew.moe_quantize_w4(wf)
+        y = ew.moe_grouped_gemm_w4(x, 1, N, P, c.cuda(), off.cuda(), por.cuda(), packed)
+        y2 = ew.moe_grouped_gemm_w4(x, 1, N, P, c2.cuda(), off2.cuda(), back.to(torch.int32).cuda(), packed.flip(0).contiguous())
+        assert torch.equal(y2.flip(0), y)
