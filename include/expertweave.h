@@ -429,7 +429,8 @@ int moe_grouped_gemm(const void* x, int dtype, int num_tokens, int num_rows, int
  *   dy [dev] dtype [num_rows, N]; x [dev] dtype [num_tokens, K]
  *   dw [dev] dw_dtype [num_slots, N, K]: EW_F32, or EW_BF16 for bf16 rows (rounded once).  accumulate != 0
  *      adds to what dw holds (EW_F32 only); otherwise slots without rows get zeros.
- * A product of the second form (transposed != 0) has the same gradient with dy and x exchanged.  Matrix cores:
+ * A product of the second form (transposed != 0) has the same gradient with dy and x exchanged (pair_of_row NULL,
+ * k = 1) where its x is in sorted rows; rows of dy are never looked up, so a gathered x has to be sorted first.  Matrix cores:
  * as above, the slots' rows addressable with 32-bit byte offsets, and K <= 32000 where rows of x are looked up.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 int moe_grouped_gemm_wgrad(const void* dy, const void* x, int dtype, int num_tokens, int num_rows, int k, int K,

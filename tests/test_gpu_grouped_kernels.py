@@ -141,3 +141,14 @@ def test_a_rows_bits_do_not_depend_on_its_place(ew, K, N, dtype, counts):
         y = ew.moe_grouped_gemm_w4(x, 1, N, P, c.cuda(), off.cuda(), por.cuda(), packed)
         y2 = ew.moe_grouped_gemm_w4(x, 1, N, P, c2.cuda(), off2.cuda(), back.to(torch.int32).cuda(), packed.flip(0).contiguous())
         assert torch.equal(y2.flip(0), y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weight_gradient_of_the_transposed_product(ew, dtype):
+    """y = W^T x with x in sorted rows: dW[k][n] = sum_r x[r][k] dy[r][n] is the weight gradient with dy and x exchanged."""
+    g, counts, K, N = gen(47), [0, 3, 70, 129, 0, 300], 136, 264
+    c, off, _, tok, tokens = ref.rows_of(counts, g, k=1, shuffled=False)
+    x, dy = normal(g, tokens, K, dtype=dtype), normal(g, tokens, N, dtype=dtype)
+    dw = ew.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), 1, len(counts), c.cuda(), off.cuda(), None)
+    assert dw.shape == (len(counts), K, N)
+    close(dw, ref.wgrad(x.double(), dy.double(), off, False))
