@@ -73,11 +73,12 @@ class MoELayer:
         self.w13_base, self.w2_base, self.emap, _ = pool.view(layer)
         self.H = Wg.shape[1]
         # A layer pass reads experts of its own type, one right behind the other: a pool of another type's experts, or of 4-bit ones, would
-        # be read as noise and past its end.
+        # be read as noise and past its end.  (Whatever else has M, N, P and view() may serve as a pool, and answers for its sizes itself.)
         el = torch.empty(0, dtype=dtype).element_size()
-        if (pool.w13_bytes, pool.w2_bytes) != (2 * I * self.H * el, self.H * I * el):
-            raise ValueError(f"the pool's experts have {pool.w13_bytes} + {pool.w2_bytes} bytes, a layer of {dtype}, H={self.H}, I={I} reads "
-                             f"{2 * I * self.H * el} + {self.H * I * el}")
+        need = (2 * I * self.H * el, self.H * I * el)
+        has = (getattr(pool, "w13_bytes", need[0]), getattr(pool, "w2_bytes", need[1]))
+        if has != need:
+            raise ValueError(f"the pool's experts have {has[0]} + {has[1]} bytes, a layer of {dtype}, H={self.H}, I={I} reads {need[0]} + {need[1]}")
         self.S = 0 if shared_w13 is None else shared_w13.shape[0]
         self.shared_w13, self.shared_w2 = shared_w13, shared_w2
         self.T_max = self._T = T_max

@@ -49,6 +49,14 @@ def test_a_layer_refuses_a_pool_of_other_experts():
         pool.close()
 
 
+def test_a_layer_takes_a_pool_that_states_no_sizes():
+    """Weights that lie elsewhere than in an ExpertPool: an object with M, N, P and view() is enough."""
+    from types import SimpleNamespace
+    from paper_2508_17624_amd.layer import MoELayer
+    pool = SimpleNamespace(M=4, N=1, P=6, view=lambda layer: (256, 512, 1024, 6))
+    assert MoELayer(pool, 0, torch.zeros(4, 64), None, None, 2, 32, 8, torch.bfloat16).w2_base == 512
+
+
 def test_a_pool_refuses_weights_shorter_than_its_experts():
     """4-bit experts handed to a bf16 pool, or too few of them, would be copied from past the end of the tensor."""
     M, H, I = 3, 64, 32
