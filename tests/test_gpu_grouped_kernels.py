@@ -103,6 +103,30 @@ def test_many_rows_that_are_not_looked_up(ew, K, N):
     products.run_gemm(ew, products.RAGGED, K, N, "fwd", "bf16", 1, False, 44)
 
 
+@pytest.mark.parametrize("H,I,counts", [(128, 128, products.RAGGED), (256, 256, [300, 0, 700])], ids=["small tiles", "large tiles"])
+def test_four_bit_ffn_of_rows_that_are_not_looked_up(ew, H, I, counts):
+    rng, g, P = np.random.default_rng(48), gen(48), len(counts)
+    p13, w13 = products.random_w4(rng, P, 2 * I, H, spread=1)
+    p2, w2 = products.random_w4(rng, P, H, I, spread=1)
+    empty = torch.tensor(counts) == 0
+    p13[empty], p2[empty] = 255, 255
+    c, off, _, tok, tokens = ref.rows_of(counts, g, k=1, shuffled=False)
+    x = normal(g, tokens, H)
+    y = ew.moe_grouped_ffn_w4(x.cuda(), 1, I, P, c.cuda(), off.cuda(), None, p13.cuda(), p2.cuda())
+    close(y, ref.ffn(x.double(), w13, w2, off, True))
+
+
+@pytest.mark.parametrize("H,I,counts", [(264, 72, products.RAGGED), (640, 264, [0, 300, 129, 0, 1, 1])], ids=["small tiles", "large tiles"])
+def test_ffn_gradients_of_rows_that_are_not_looked_up(ew, H, I, counts):
+    g, P = gen(49), len(counts)
+    c, off, _, tok, tokens = ref.rows_of(counts, g, k=1, shuffled=False)
+    x, dy = normal(g, tokens, H), normal(g, tokens, H, std=0.5)
+    w13, w2 = normal(g, P, 2 * I, H, std=H ** -0.5), normal(g, P, H, I, std=I ** -0.5)
+    got = ew.moe_grouped_ffn_backward(x.cuda(), dy.cuda(), 1, I, P, c.cuda(), off.cuda(), None, products.poison(w13, counts).cuda(), products.poison(w2, counts).cuda())
+    for name, a, b in zip(("dx", "dw13", "dw2"), got, bounds.ffn_backward(x.double(), dy.double(), w13.double(), w2.double(), off, True, False)):
+        close(a, b, name)
+
+
 def test_four_bit_tiles_keep_scales_of_255_to_their_feature(ew):
     """As the few-row kernels: one output is NaN in every row, the others are as without it."""
     K, N, counts = 128, 32, [300, 0, 90]
