@@ -631,10 +631,10 @@ bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   if (weights == kW4 ? way != kFwd || a.K % 128 || a.N % 16 : weights != kWBf16 || a.K % 8 || a.N % 8) return false;
   if (epilogue == kEpSwiglu && weights != kW4) return false;
   if (epilogue == kEpBack && (weights == kW4 || way != kFwd)) return false;
-  if (epilogue == kEpF32 && way == kFwd) return false;  // (nobody asks for these)
+  const bool mapped = a.g.por != nullptr || a.g.k > 1;
+  if (epilogue == kEpF32 && (way == kFwd || (way == kDgrad && mapped))) return false;  // (nobody asks for these)
   if (!aligned16(a.x) || !aligned16(a.w) || !aligned16(a.out)) return false;
   if (epilogue == kEpBack && (!aligned16(a.da) || !aligned16(a.dh))) return false;
-  const bool mapped = a.g.por != nullptr || a.g.k > 1;
   // byte offsets are 32 bits wide: into a slot's weights and the looked-up rows, and into one slot's rows where they are the contraction
   const unsigned long long x_bytes = (unsigned long long)a.x_rows * a.K * 2, row_bytes = (unsigned long long)a.g.rows * (a.N > a.K ? a.N : a.K) * 2;
   if (mapped && x_bytes >= lim - 65536) return false;
@@ -645,7 +645,7 @@ bool tile_takes(int way, int weights, int epilogue, const GemmArgs& a) {
 int launch_tile(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st) {
   if (weights == kW4) return epilogue == kEpSwiglu ? launch_mapped<kFwd, kEpSwiglu, true>(a, st) : launch_mapped<kFwd, kEpBf16, true>(a, st);
   if (way == kDgrad) {
-    if (epilogue == kEpF32) return launch_mapped<kDgrad, kEpF32>(a, st);
+    if (epilogue == kEpF32) return launch_sized<kDgrad, kEpF32, false, false>(a, st);
     return launch_mapped<kDgrad, kEpBf16>(a, st);
   }
   if (way == kWgrad) return epilogue == kEpF32 ? launch_mapped<kWgrad, kEpF32>(a, st) : launch_mapped<kWgrad, kEpBf16>(a, st);
