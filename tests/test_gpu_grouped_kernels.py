@@ -176,3 +176,65 @@ def test_weight_gradient_of_the_transposed_product(ew, dtype):
     dw = ew.moe_grouped_gemm_wgrad(x.cuda(), dy.cuda(), 1, len(counts), c.cuda(), off.cuda(), None)
     assert dw.shape == (len(counts), K, N)
     close(dw, ref.wgrad(x.double(), dy.double(), off, False))
+
+
+# ------------------------------------------------------------------------------------------------ nothing, and a lot
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mapped", [True, False])
+def test_calls_without_rows(ew, mapped, dtype):
+    """No token at all, and tokens without a row: empty results, zero gradients, sums kept."""
+    P, H, I, dt = 5, 128, 64, products.DT[dtype]
+    zero = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")
+    w13, w2 = (torch.full(s, float("nan"), dtype=dt, device="cuda") for s in ((P, 2 * I, H), (P, H, I)))
+    for T in (0, 3):
+        x, none = torch.ones((T, H), dtype=dt, device="cuda"), torch.empty((0, H), dtype=dt, device="cuda")
+        at = (P, zero(P), zero(P + 1), zero(0) if mapped else None)
+        assert ew.moe_grouped_gemm(x, 2, 2 * I, *at, w13, num_rows=0).shape == (0, 2 * I)
+        assert not ew.moe_grouped_gemm_wgrad(none, x, 2, *at).any()
+        kept = ew.moe_grouped_gemm_wgrad(none, x, 2, *at, accumulate=True, out=torch.full((P, H, H), 3.0, device="cuda"))
+        assert (kept == 3).all()
+        dx, d13, d2 = ew.moe_grouped_ffn_backward(x, none, 2, I, *at, w13, w2)
+        assert dx.shape == (0, H) and d13.shape == w13.shape and d2.shape == w2.shape and not d13.any() and not d2.any()
+        if dtype == "bf16":
+            packed = torch.full((P, ew.moe_w4_expert_bytes(2 * I, H)), 255, dtype=torch.uint8, device="cuda")
+            assert ew.moe_grouped_gemm_w4(x, 2, 2 * I, *at, packed, num_rows=0).shape == (0, 2 * I)
+            assert ew.moe_grouped_ffn_w4(x, 2, I, *at, packed, packed, num_rows=0).shape == (0, H)
+    # room for rows, none of them there
+    out = torch.full((6, 2 * I), 7.0, dtype=dt, device="cuda")
+    ew.moe_grouped_gemm(x, 2, 2 * I, P, zero(P), zero(P + 1), zero(6) if mapped else None, w13, out=out, num_rows=6)
+    assert (out == 7).all()
+    dy, dw = ew.moe_unpermute_backward(torch.empty((0, H), dtype=dt, device="cuda"), zero(0), torch.empty((0, 2), device="cuda"), torch.empty((0, H), dtype=dt, device="cuda"))
+    assert dy.shape == (0, H) and dw.shape == (0, 2)
+    assert ew.moe_quantize_w4(torch.empty((0, 16, 64), dtype=dt, device="cuda")).shape == (0, ew.moe_w4_expert_bytes(16, 64))
+
+
+def test_results_and_packed_experts_beyond_4_gib(ew):
+    """Weight gradients and 4-bit experts whose slots lie further from the base than 32 bits reach."""
+    g, N, K = gen(50), 2816, 2816
+    P, at = 300, ((0, 5), (290, 40), (299, 130))
+    counts = [0] * P
+    for s, n in at:
+        counts[s] = n
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=2)
+    x, dy = normal(g, tokens, K), normal(g, len(tok), N)
+    dw = ew.moe_grouped_gemm_wgrad(dy.cuda(), x.cuda(), 2, P, c.cuda(), off.cuda(), por.cuda(), dtype=torch.bfloat16)   # 4.8 GB
+    for s, i, j in ref.slots_of(off):
+        close(dw[s:s + 1], ref.wgrad(dy.double()[i:j], x.double()[tok[i:j]], torch.tensor([0, j - i]), True), f"slot {s}")
+        dw[s] = 0
+    assert not any(dw[i:i + 10].any() for i in range(0, P, 10)), "slots without rows"
+    del dw
+    P, at = 1200, ((0, 3), (1100, 20), (1199, 260))                                                                    # 5.1 GB
+    counts = [0] * P
+    for s, n in at:
+        counts[s] = n
+    rng = np.random.default_rng(50)
+    packed = torch.full((P, ew.moe_w4_expert_bytes(N, K)), 255, dtype=torch.uint8, device="cuda")
+    values = {}
+    for s, _ in at:
+        one, values[s] = products.random_w4(rng, 1, N, K)
+        packed[s] = one[0].cuda()
+    c, off, por, tok, tokens = ref.rows_of(counts, g, k=2)
+    x = normal(g, tokens, K)
+    y = ew.moe_grouped_gemm_w4(x.cuda(), 2, N, P, c.cuda(), off.cuda(), por.cuda(), packed, num_rows=len(tok))
+    for s, i, j in ref.slots_of(off):
+        close(y[i:j], ref.gemm(x.double()[tok[i:j]], values[s], torch.tensor([0, j - i]), True), f"4 bits, slot {s}")
