@@ -6,8 +6,10 @@
 //     dx  = W1g^T dg + W1u^T du         dW13 = sum_r [dg; du] x^T
 // g and u are computed again: kept from the forward pass they would be 2 I values a row for as long as the layers behind this one run.
 // da comes first, in fp32; the product that makes g and u then forms dg, du and a in its epilogue, where a lane holds both of a feature.  Of what
-// lies between the products only dg, du and a are rounded to bf16, as operands of the matrix cores.  (With g, u and da in bf16 too the
-// gradients' relative error is 3.5e-3 instead of 2.4e-3.)
+// lies between the products only dg, du and a are rounded to bf16, as operands of the matrix cores: the gradients are 2.3e-3 from 64 bits in bf16, where
+// the rounding of the results alone is 1.7e-3.  (With g, u and da in bf16 too 3.5e-3.)
+// fp32: 8 slots of 512 rows, 2048 x 1408, 1884 us (100 TFLOP/s of the 140 that a large library product reaches); configuration 0's layer, 16 slots of 8
+// rows, 256 x 128, 44 us, five launches one after the other.
 #include "grouped_gemm.h"
 
 namespace ew {

@@ -10,9 +10,10 @@
 //           and v_cvt_scalef32_pk_bf16_fp4 makes two bf16 values of them at a time, exactly, scale included; a row's scales of all
 //           four blocks are one load
 // and x is loaded to match (any order of the contraction will do as long as both operands have the same).
-// What bounds the 4-bit stream is not bytes but load instructions.  A kernel whose waves walked over the whole contraction, loading x and
-// scales block by block (three loads per strip and block instead of 1.25), took 163 us for both products of the FFN at 64 tokens on 20 adapters of 2048 x
-// 1408 (501 MB); without its loads of scales 126, without those of x too 110, which is what this one takes (4.5 TB/s).
+// Both products of the FFN in 4 bits take 68 + 42 us at 64 tokens on 20 adapters of 2048 x 1408 (501 MB, 4.5 TB/s); the first product in bf16, four
+// adapters, 165 (933 MB, 5.6 TB/s).  What keeps the 4-bit stream from the other's rate is in part the loads of scales, one load in five, of which
+// the four lanes of a feature fetch the same 16 bytes: without them 64 + 36; without the conversion it takes as long as with it.  (Waves that walked
+// over the whole contraction, loading x and scales block by block, three loads per strip and block instead of 1.25, took 163 for both.)
 #include "grouped_gemm.h"
 
 #include <type_traits>
@@ -68,7 +69,10 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 template <int WT_, int NW_, int TL_, int EP_, int R_, int D_, int WPE_>
 struct Cfg {
   static constexpr int WT = WT_, NW = NW_, TL = TL_, EP = EP_, R = R_, D = D_, WPE = WPE_;
-  static constexpr int XB = 4;                    // blocks of the contraction that a wave holds of x
+  // Blocks of the contraction that a wave holds of x: 64 registers a row tile, beside as many of a bf16 strip.  For bf16 that ends at K = 2048 with four
+  // waves; eight are slower than the tiles (64 slots of 2816 features, 1 to 6 rows, eight waves / tiles, us: K = 2560 196 to 202 / 164 to 165, 4096 265
+  // to 271 / 252 to 256; at 2048, four waves: 128 to 135 / 142 to 143).
+  static constexpr int XB = 4;
   static constexpr bool GATED = EP == kEpSwiglu;  // strips come in pairs, gate and up
 };
 template <int WT>
@@ -247,7 +251,11 @@ bool stream_takes(int way, int weights, int epilogue, const GemmArgs& a) {
   if (a.slot_bytes >= lim) return false;
   // What the waves of a workgroup can hold of x, and where it is faster than the tiles: us, 64 slots of 2048 x 1408 with so many rows, this kernel / tiles:
   // 4 bits, both products: 16 81 / 129, 32 105 / 132, 48 161 / 145; bf16, first product: 4 134 / 141, 12 142 / 143, 24 155 / 146 (weights of
-  // 16 slots, which the memory-side cache holds: 4 33 / 30).  The host knows the average over all slots; those in use have more.
+  // 16 slots, which the memory-side cache holds: 4 33 / 30).
+  // The host knows the average over all slots, and these lines hold where all are in use.  Slots without rows move them: the same 64 slots of base experts in a
+  // pool of 384 take the stream up to six times as many rows per slot in use.  This kernel / tiles there, us: 4 bits 24 116 / 148, 48 167 / 161, 94 296 /
+  // 182, 188 382 / 318 (a pool of 64: 100, 150, 169, 241); bf16 6 163 / 152, 24 159 / 155 (130, 148).  Counts are on the device, where nothing
+  // chooses between kernels.
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;
   // Beyond K = 4096 one tile of 16 rows is all that fits beside the partial sums, and 32 rows would read the weights twice: 8192 x 1024, 64
   // slots: 16 rows 93 / 106, 32 rows 169 / 110 (both products with a hidden size of 8192: 222 / 333 at 16 rows).
@@ -258,6 +266,9 @@ bool stream_takes(int way, int weights, int epilogue, const GemmArgs& a) {
 int launch_stream(int way, int weights, int epilogue, const GemmArgs& a, hipStream_t st) {
   (void)way;
   if (weights == kW4) return epilogue == kEpSwiglu ? launch_w4_waves<kEpSwiglu>(a, st) : launch_w4_waves<kEpBf16>(a, st);
+  // Two row tiles where a slot can have many rows: slots of 17 to 32 read their weights once (64 slots in use of 384, 24 rows each: one tile 262 us, two 159).
+  // Spread evenly, up to 6 rows a slot, one tile is up to 4 % faster (2048 x 2816, us: 128 slots 226 rows 219 / 218, 506 246 / 256, 773 283 / 288; 384 slots
+  // 1572 rows 716 / 727; with fewer tokens 0 to 9 %).
   const int tokens = a.g.por || a.g.k > 1 ? a.x_rows : a.g.rows, strips = ceil_div(a.N, 16);
   if (tokens <= 64) return launch_cfg<kWBf16, 4, 1, kEpBf16, 2, 1, 3>(a, strips_per_group(a, strips, 4), st);
   return launch_cfg<kWBf16, 4, 2, kEpBf16, 2, 1, 2>(a, strips_per_group(a, strips, 16), st);

@@ -307,6 +307,9 @@ __global__ __launch_bounds__(C::THREADS) __attribute__((amdgpu_waves_per_eu(C::W
   // scale.  The even slab of the two takes the first half of every group, the odd one the second (x is loaded to match), so all lanes turn
   // half of what they hold into bf16 in LDS, a slab ahead of its use.  (A lane with 32 bytes of a feature of its own instead, a slab's worth,
   // touches 64 lines per load instruction: 64 slots of 16 rows, both products of the FFN, 161 us instead of 147.)
+  // Codes are asked for two to four slabs before their use but are only one slab in flight: outstanding loads are counted in order, and the wait for the
+  // rows of a slab is a wait for the codes before them.  What the 4-bit form costs, 3999 tokens on 20 adapters of 2048 x 1408, both kernels: 513 + 278 us,
+  // without the conversion 496 + 267, without the LDS writes of its results either 451 + 248 (a quarter of the LDS cycles are bank conflicts there).
   u32x4 codes[C::RW], codes_next[C::RW];
   uint32_t scales[C::RW] = {}, scales_next[C::RW] = {}, w4_codes[C::RW], w4_scales[C::RW];
   if constexpr (C::W4) {
@@ -612,7 +615,11 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // The larger tile where a slot has many rows on average (the weight gradient: wherever the outputs fill it).  Both sides, us, 64 slots of 2048 x
 // 1408 with so many rows, small / large tile: bf16, first product: 48 154 / 154, 96 171 / 166, 192 237 / 188; 4 bits, both products: 64 146 / 165,
-// 128 188 / 203, 192 297 / 240.
+// 128 188 / 203, 192 297 / 240.  The average is over all slots, those without rows too: 64 slots of 188 rows each get the small tile in a pool of 384 (bf16
+// 246 instead of 190, 4 bits 318 instead of 241).
+// Weight gradient in fp32 (bf16), 64 slots, small / large, at 32, 125 and 768 rows a slot: 512 x 512 16 / 15, 18 / 17, 40 / 39; 640 x 640 23 / 25, 26 / 30,
+// 62 / 66 (17 / 22, 19 / 26, 50 / 63); 1024 x 512 26 / 28, 29 / 31, 83 / 68; 1536 x 640 51 / 48, 60 / 59, 155 / 138 (30 / 34, 34 / 39, 131 / 120); 2048 x 1408
+// 141 / 131, 186 / 171, 439 / 350: between 512 x 512 and 1024 x 640 few rows would rather have the small one.
 template <int WAY, int EP, bool MAPPED, bool W4>
 int launch_sized(const GemmArgs& a, hipStream_t st) {
   const long long used = a.g.P < a.g.rows ? a.g.P : a.g.rows;

@@ -180,6 +180,8 @@ extern "C" int moe_grouped_ffn_w4(const void* x, int num_tokens, int num_rows, i
   const size_t need = moe_grouped_ffn_w4_workspace_bytes(num_rows, I);
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < need)
     return fail(EW_ERR_WORKSPACE, "%s: workspace needs %zu bytes aligned to 256 (got %zu at %p)", who, need, ws_bytes, ws);
+  // The activation is bf16 between the products, as in moe_grouped_ffn: it is the second one's operand on the bf16 matrix cores.  (2.3e-3 from 64 bits;
+  // an activation in fp32 would leave the rounding of y, 1.7e-3.)
   const hipStream_t st = (hipStream_t)stream;
   const int rc = ew::launch_gemm(ew::kFwd, ew::kW4, ew::kEpSwiglu, true,
                                  w4_args(counts, offsets, pair_of_row, P, num_rows, k, x, num_tokens, w13_base, ws, H, I, moe_w4_expert_bytes(2 * I, H)), st);
